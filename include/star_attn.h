@@ -353,6 +353,125 @@ int star_attn_rope(const star_attn_shape* shape, int32_t n_heads, int64_t n_toke
                    double rope_theta, const void* X, void* Y, void* hip_stream);
 
 /*
+ * Queries and keys that are normed per head before they are rotated, and positions on
+ * several axes.
+ *
+ * A head's row x of d elements is divided by its root mean square and weighted,
+ *     n_i = x_i w_i / sqrt(mean(x^2) + norm_eps),
+ * and then rotated as above, frequency i by the angle p_i * rope_theta^(-2i/d), where p_i is
+ * the token's position on the axis that has frequency i (time, height and width of a
+ * video's patch, for instance).  Sums, norms and the rotation run in fp32, angles in
+ * double precision; the result is rounded once to the storage dtype.  Every element of
+ * the row takes part, so a row that holds a NaN or an infinity comes out as NaN.
+ */
+typedef struct star_attn_rotary {
+  double rope_theta;         /* base of the frequencies, > 1 */
+  int64_t pos0;              /* without `positions`: token t of phase 1 sits at pos0 + t, new token j
+                                of phase 2 at pos0 + cache_len + j, on every axis; >= 0 */
+  const int64_t* positions;  /* device [B, n_tokens, n_axes], the call's tokens; any value up to 2^40
+                                in size; NULL: see pos0 */
+  const void* q_norm;        /* device [d] in the storage dtype: w of the queries, NULL: not normed */
+  const void* k_norm;        /* the same for the keys */
+  float norm_eps;            /* >= 0 */
+  int32_t n_axes;            /* 1 to 4 */
+  uint8_t axis[64];          /* axis of frequency i < d / 2, below n_axes */
+} star_attn_rotary;
+
+/*
+ * star_attn_qk_norm_rope: the pass alone, for both in one launch.
+ *   Q, Yq      [B, n_tokens, Hq, d]    Yq may be Q; both may be NULL
+ *   K, Yk      [B, n_tokens, Hkv, d]   Yk may be K; both may be NULL, if Q is not
+ * star_attn_phase1_norm_rope / star_attn_phase2_norm_rope: star_attn_phase1_rope /
+ * star_attn_phase2_rope with `rotary` in place of rope_theta and pos0.  A rotary out of
+ * range is STAR_ATTN_ERR_INVALID_SHAPE, positions or weights that are not 16-byte aligned
+ * are STAR_ATTN_ERR_MISALIGNED.
+ */
+int star_attn_qk_norm_rope(const star_attn_shape* shape, const star_attn_rotary* rotary, int64_t n_tokens,
+                           const void* Q, const void* K, void* Yq, void* Yk, void* hip_stream);
+
+int star_attn_phase1_norm_rope(const star_attn_shape* shape, const star_attn_rotary* rotary,
+                               void* Q, const void* K, const void* V,
+                               void* O_ctx, float* LSE_ctx,
+                               void* K_cache, void* V_cache,
+                               void* workspace, size_t workspace_bytes, void* hip_stream);
+
+int star_attn_phase2_norm_rope(const star_attn_shape* shape, const star_attn_rotary* rotary,
+                               int64_t cache_len, int64_t q_len,
+                               void* Qq, const void* Kq, const void* Vq,
+                               void* K_cache, void* V_cache,
+                               float* O_part, float* LSE_part,
+                               void* O,
+                               void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * A cache held in four bits: 4.25 bits an element, for contexts whose cache is what a step
+ * waits for, or what does not fit.
+ *
+ * A row of d elements is d / 32 groups.  A group is 32 codes and one exponent byte e, its
+ * unit 2^(e - 127): the largest power of two u with 3.5 u <= max |x|, from 2^-125 to 2^125.  A code
+ * stands for its sign (bit 3) times 0, .5, 1, 1.5, 2, 3, 4, 6 (bits 0 to 2) units, and is
+ * the nearest of these to the element (the even code of two as near): off by a quarter of a unit for
+ * small elements and by at most one, a fifth of the group's largest element, between 4 and 7 units.
+ * e = 255 marks a group that held a NaN or an infinity; all of it reads as NaN.
+ *
+ * All four pointers are device memory, 16-byte aligned:
+ *   k_codes, v_codes    [B, Hkv, cache_capacity, d / 2] bytes, element 2k in the low half of byte k
+ *   k_scales, v_scales  [B, Hkv, cache_capacity, d / 32] bytes
+ */
+typedef struct star_attn_q4_cache {
+  void* k_codes;
+  void* k_scales;
+  void* v_codes;
+  void* v_scales;
+} star_attn_q4_cache;
+
+/*
+ * star_attn_q4_store: rows [plain_row, plain_row + n_rows) of K and V [B, Hkv, plain_rows, d]
+ * in the storage dtype (for a cache that phase 1 has filled, plain_rows = cache_capacity) become
+ * rows [first_row, first_row + n_rows) of the four-bit cache.
+ * star_attn_q4_load: the same rows back, exactly what their codes stand for.
+ * n_rows >= 1; rows past either capacity are STAR_ATTN_ERR_CACHE_OVERFLOW; B * Hkv * n_rows is
+ * below 2^31.  No other row is touched.
+ */
+int star_attn_q4_store(const star_attn_shape* shape, int64_t first_row, int64_t n_rows,
+                       const void* K, const void* V, int64_t plain_rows, int64_t plain_row,
+                       const star_attn_q4_cache* cache, void* hip_stream);
+
+int star_attn_q4_load(const star_attn_shape* shape, int64_t first_row, int64_t n_rows,
+                      const star_attn_q4_cache* cache, void* K, void* V, int64_t plain_rows,
+                      int64_t plain_row, void* hip_stream);
+
+/*
+ * star_attn_phase2_q4: star_attn_phase2 over a four-bit cache.  The new tokens' K and V are
+ * filed in it first, and attention is defined on what the cache then holds: the values its
+ * codes stand for, the new tokens' among them, against Qq as it is.  A NaN counts for the rows
+ * that see its key and for no other.
+ *   rotary     NULL: Qq and Kq are taken as they are.  Else they are unrotated: Qq is normed and
+ *              rotated IN PLACE, Kq on its way into the cache (rounded to the storage dtype
+ *              before it is put into four bits), as in star_attn_phase2_norm_rope
+ *   workspace  at least star_attn_q4_workspace_bytes(shape, q_len) bytes, 256-byte aligned
+ * Other arguments, outputs (O_part, LSE_part, O) and errors as in star_attn_phase2.
+ * star_attn_phase2_q4_partial: star_attn_phase2_partial over a four-bit cache, one host's pair
+ * (A, LSE) for star_attn_merge; Kq and Vq both NULL for a context host.
+ * star_attn_phase2_q4_plan: what a star_attn_phase2_q4 call would run (see star_attn_phase2_plan).
+ */
+size_t star_attn_q4_workspace_bytes(const star_attn_shape* shape, int64_t max_q_len);
+
+int star_attn_phase2_q4(const star_attn_shape* shape, const star_attn_rotary* rotary,
+                        int64_t cache_len, int64_t q_len,
+                        void* Qq, const void* Kq, const void* Vq,
+                        const star_attn_q4_cache* cache,
+                        float* O_part, float* LSE_part,
+                        void* O,
+                        void* workspace, size_t workspace_bytes, void* hip_stream);
+
+int star_attn_phase2_q4_partial(const star_attn_shape* shape, int64_t cache_len, int64_t q_len,
+                                const void* Qq, const void* Kq, const void* Vq,
+                                const star_attn_q4_cache* cache,
+                                float* A, float* LSE,
+                                void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
  * What a star_attn_phase2 call with these arguments would run (Section 2.2: how the
  * cache is cut into the pieces whose pairs (A, lse) of Eq. 1-2 are merged by Eq. 3-4).
  * For logs, benchmarks and tests that must know which kernel set-up they exercised.
@@ -378,6 +497,9 @@ typedef struct star_attn_plan_info {
 
 int star_attn_phase2_plan(const star_attn_shape* shape, int64_t cache_len, int64_t q_len,
                           int want_parts, star_attn_plan_info* out);
+
+int star_attn_phase2_q4_plan(const star_attn_shape* shape, int64_t cache_len, int64_t q_len,
+                             int want_parts, star_attn_plan_info* out);
 
 /* The same for a star_attn_phase1 / _anchor / _rope call: which set-up takes it. */
 typedef struct star_attn_phase1_plan_info {

@@ -10,4 +10,6 @@ from .binding import (  # noqa: F401
     StarAttnError, StarShape, lib_path, load_library, phase1, phase1_anchor, phase1_rope,
     phase1_workspace_bytes, phase2, phase2_partial, phase2_rope, merge, rope, status_string,
     workspace_bytes, kernel_path, alloc_cache, alloc_workspace, phase1_plan, phase2_plan, PlanInfo, phase2_static, STATIC_SCRATCH_BYTES,
+    Rotary, qk_norm_rope, phase1_norm_rope, phase2_norm_rope, Q4Cache, alloc_q4_cache, q4_workspace_bytes, alloc_q4_workspace,
+    q4_store, q4_load, phase2_q4, phase2_q4_partial, phase2_q4_plan,
 )

@@ -54,6 +54,93 @@ class StarShape(ctypes.Structure):
                    float(softmax_scale), 0.0)
 
 
+class StarRotary(ctypes.Structure):
+    """Mirror of `star_attn_rotary`."""
+    _fields_ = [
+        ("rope_theta", ctypes.c_double), ("pos0", ctypes.c_int64), ("positions", ctypes.c_void_p),
+        ("q_norm", ctypes.c_void_p), ("k_norm", ctypes.c_void_p), ("norm_eps", ctypes.c_float),
+        ("n_axes", ctypes.c_int32), ("axis", ctypes.c_uint8 * 64),
+    ]
+
+
+def _pointer(t, what, dtype=None, shape=None):
+    if t is None:
+        return None
+    if not t.is_contiguous():
+        raise ValueError("star_attn tensors must be contiguous")
+    if (dtype is not None and t.dtype != dtype) or (shape is not None and tuple(t.shape) != tuple(shape)):
+        raise ValueError(f"{what}: {tuple(t.shape)} {t.dtype} given" + (f", {tuple(shape)} wanted" if shape else ""))
+    return t.data_ptr()
+
+
+class Rotary:
+    """How a call's queries and keys are normed per head and rotated (`star_attn_rotary`); holds on to its tensors.
+
+    q_norm, k_norm: weights [d] in the storage dtype, None: not normed.  positions: int64 [B, n_tokens, n_axes] (or [B,
+    n_tokens]) of the call's tokens, None: they follow each other from pos0 on (in phase 2 behind the cache).  sections: how many of
+    the d / 2 frequencies each axis turns, one after the other; or `axis`: every frequency's axis."""
+
+    def __init__(self, rope_theta: float, q_norm=None, k_norm=None, eps: float = 1e-6, pos0: int = 0, positions=None,
+                 sections=None, axis=None):
+        if sections is not None and axis is not None:
+            raise ValueError("sections or axis, not both")
+        if sections is not None:
+            axis = [a for a, n in enumerate(sections) for _ in range(n)]
+        axes = [0] if axis is None else [int(a) for a in axis]
+        n_axes = len(sections) if sections is not None else max(axes) + 1
+        if positions is not None:
+            n_axes = max(n_axes, positions.shape[2]) if positions.dim() == 3 else 1
+            if positions.dim() not in (2, 3) or (positions.dim() == 3 and positions.shape[2] != n_axes) or max(axes) >= n_axes:
+                raise ValueError("positions are [batch, tokens, axes]")
+        if axis is not None and (len(axes) not in (32, 64) or min(axes) < 0):
+            raise ValueError("an axis for each of the d / 2 frequencies is wanted")
+        for w in (q_norm, k_norm):
+            if w is not None and w.dim() != 1:
+                raise ValueError("norm weights are [head_dim]")
+        self.tensors = (q_norm, k_norm, positions)
+        self.frequencies = None if axis is None else len(axes)
+        self.c = StarRotary(float(rope_theta), int(pos0), _pointer(positions, "positions", torch.int64), _pointer(q_norm, "q_norm"),
+                            _pointer(k_norm, "k_norm"), float(eps), n_axes, (ctypes.c_uint8 * 64)(*axes))
+
+
+    def of(self, shape: StarShape, n_tokens: int) -> StarRotary:
+        """The struct, for a call of that shape."""
+        q_norm, k_norm, positions = self.tensors
+        d, size = shape.head_dim, 4 if shape.dtype == F32 else 2
+        for w in (q_norm, k_norm):
+            if w is not None and (w.shape[0] != d or w.element_size() != size):
+                raise ValueError("norm weights are [head_dim] in the storage dtype")
+        if positions is not None and tuple(positions.shape[:2]) != (shape.batch, n_tokens):
+            raise ValueError(f"positions of {tuple(positions.shape[:2])} tokens given, {(shape.batch, n_tokens)} wanted")
+        if self.frequencies not in (None, d // 2):
+            raise ValueError("an axis for each of the d / 2 frequencies is wanted")
+        return self.c
+
+
+class StarQ4(ctypes.Structure):
+    """Mirror of `star_attn_q4_cache`."""
+    _fields_ = [("k_codes", ctypes.c_void_p), ("k_scales", ctypes.c_void_p), ("v_codes", ctypes.c_void_p), ("v_scales", ctypes.c_void_p)]
+
+
+class Q4Cache:
+    """A cache held in four bits (`star_attn_q4_cache`): uint8 codes [B, Hkv, cache_capacity, d / 2] and exponents
+    [B, Hkv, cache_capacity, d / 32] of K and of V, the caller's tensors (alloc_q4_cache makes them)."""
+
+    def __init__(self, shape: StarShape, k_codes, k_scales, v_codes, v_scales):
+        rows = (shape.batch, shape.n_kv_heads, shape.cache_capacity)
+        sizes = {"codes": rows + (shape.head_dim // 2,), "scales": rows + (shape.head_dim // 32,)}
+        self.rows, self.head_dim = rows, shape.head_dim
+        self.k_codes, self.k_scales, self.v_codes, self.v_scales = k_codes, k_scales, v_codes, v_scales
+        self.c = StarQ4(*(_pointer(getattr(self, n), n, torch.uint8, sizes[n[2:]]) for n, _ in StarQ4._fields_))
+
+
+    def of(self, shape: StarShape) -> StarQ4:
+        """The struct, for a call of that shape."""
+        if self.rows != (shape.batch, shape.n_kv_heads, shape.cache_capacity) or self.head_dim != shape.head_dim:
+            raise ValueError(f"a four-bit cache of {self.rows} rows of {self.head_dim} given to a call of another shape")
+        return self.c
+
+
 class PlanInfo(ctypes.Structure):
     """Mirror of `star_attn_plan_info`."""
     _fields_ = [
@@ -119,6 +206,20 @@ def load_library():
     lib.star_attn_phase2_plan.argtypes = [P, i64, i64, ctypes.c_int, ctypes.POINTER(PlanInfo)]
     lib.star_attn_phase1_plan.restype = ctypes.c_int
     lib.star_attn_phase1_plan.argtypes = [P, ctypes.c_int, ctypes.POINTER(Phase1PlanInfo)]
+    R, C4 = ctypes.POINTER(StarRotary), ctypes.POINTER(StarQ4)
+    for name, kinds in {
+            "qk_norm_rope": [P, R, i64, vp, vp, vp, vp, vp],
+            "phase1_norm_rope": [P, R, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp],
+            "phase2_norm_rope": [P, R, i64, i64, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp],
+            "q4_store": [P, i64, i64, vp, vp, i64, i64, C4, vp],
+            "q4_load": [P, i64, i64, C4, vp, vp, i64, i64, vp],
+            "phase2_q4": [P, R, i64, i64, vp, vp, vp, C4, vp, vp, vp, vp, sz, vp],
+            "phase2_q4_partial": [P, i64, i64, vp, vp, vp, C4, vp, vp, vp, sz, vp],
+            "phase2_q4_plan": [P, i64, i64, ctypes.c_int, ctypes.POINTER(PlanInfo)]}.items():
+        getattr(lib, "star_attn_" + name).restype = ctypes.c_int
+        getattr(lib, "star_attn_" + name).argtypes = kinds
+    lib.star_attn_q4_workspace_bytes.restype = sz
+    lib.star_attn_q4_workspace_bytes.argtypes = [P, i64]
     lib.star_attn_kernel_path.restype = ctypes.c_char_p
     lib.star_attn_kernel_path.argtypes = [P]
     _LIB = lib
@@ -140,21 +241,29 @@ def _bind(lib) -> None:
         module = _MARSHAL
     names = ("phase1", "phase1_anchor", "phase1_rope", "phase2", "phase2_rope", "phase2_static",
              "phase2_partial", "merge", "rope")
-    module.bind(StarShape, tuple(ctypes.cast(getattr(lib, "star_attn_" + n), ctypes.c_void_p).value
-                                 for n in names))
+    q4_names = ("qk_norm_rope", "phase1_norm_rope", "phase2_norm_rope", "q4_store", "q4_load", "phase2_q4", "phase2_q4_partial")
+    addresses = lambda names: tuple(ctypes.cast(getattr(lib, "star_attn_" + n), ctypes.c_void_p).value for n in names)
+    module.bind(StarShape, addresses(names))
+    if hasattr(lib, "star_attn_phase2_q4"):
+        module.bind_q4(addresses(q4_names))
     _MARSHAL = module
 
 
 class _CtypesCalls:
     """The extension module's calls by ctypes alone: same arguments, same refusals."""
     # what follows the shape and precedes the stream: t a tensor's address, w and its bytes, q behind its shape[1],
-    # m behind its shape[0] and shape[3]; i and d numbers
+    # m behind its shape[0] and shape[3]; i and d numbers; r a struct or None
     _KINDS = {"phase1": "tttttttw", "phase1_anchor": "itttttttttw", "phase1_rope": "ditttttttw", "phase2": "iqtttttttw",
               "phase2_rope": "diiqtttttttw", "phase2_static": "iqttttt", "phase2_partial": "iqttttttw", "merge": "mtttt"}
+    _Q4_KINDS = {"qk_norm_rope": "ritttt", "phase1_norm_rope": "rtttttttw", "phase2_norm_rope": "riqtttttttw",
+                 "phase2_q4": "riqttrtttw", "phase2_q4_partial": "iqttrttw"}
 
     def __init__(self, lib):
-        self._rope = lib.star_attn_rope
-        for name, kinds in self._KINDS.items():
+        self._rope, kinds = lib.star_attn_rope, dict(self._KINDS)
+        if hasattr(lib, "star_attn_phase2_q4"):
+            self._q4_store, self._q4_load = lib.star_attn_q4_store, lib.star_attn_q4_load
+            kinds.update(self._Q4_KINDS)
+        for name, kinds in kinds.items():
             setattr(self, name, self._entry(getattr(lib, "star_attn_" + name), kinds))
 
     @staticmethod
@@ -164,6 +273,10 @@ class _CtypesCalls:
         if not t.is_contiguous():
             raise ValueError("star_attn tensors must be contiguous")
         return t.data_ptr()
+
+    @staticmethod
+    def _struct(x):
+        return None if x is None else ctypes.byref(x)
 
     def _entry(self, fn, kinds):
         def call(shape, *args):
@@ -176,7 +289,7 @@ class _CtypesCalls:
                     out.append(x.shape[1])
                 elif kind == "m":
                     out += [x.shape[0], x.shape[3]]
-                out.append(x if kind in "id" else self._address(x))
+                out.append(x if kind in "id" else self._struct(x) if kind == "r" else self._address(x))
                 if kind == "w":
                     out.append(0 if x is None else x.numel() * x.element_size())
             return fn(*out, stream)
@@ -184,6 +297,13 @@ class _CtypesCalls:
 
     def rope(self, shape, X, Y, theta, pos0, stream):
         return self._rope(ctypes.byref(shape), X.shape[2], X.shape[1], pos0, theta, self._address(X), self._address(Y), stream)
+
+
+    def q4_store(self, shape, row, rows, K, V, plain_row, cache, stream):
+        return self._q4_store(ctypes.byref(shape), row, rows, self._address(K), self._address(V), K.shape[2], plain_row, self._struct(cache), stream)
+
+    def q4_load(self, shape, row, rows, K, V, plain_row, cache, stream):
+        return self._q4_load(ctypes.byref(shape), row, rows, self._struct(cache), self._address(K), self._address(V), K.shape[2], plain_row, stream)
 
 
 def _calls():
@@ -323,3 +443,74 @@ def phase2_partial(shape: StarShape, cache_len: int, Qq, K_cache, V_cache, A, LS
 def merge(shape: StarShape, A_parts, LSE_parts, O=None, A=None, LSE=None, stream=None) -> None:
     """star_attn_merge: Eq. 3-4 over the n_parts = A_parts.shape[0] gathered pairs."""
     _check(_calls().merge(shape, A_parts, LSE_parts, O, A, LSE, _stream(stream)))
+
+
+def qk_norm_rope(shape: StarShape, rotary: Rotary, Q, K, Yq, Yk, stream=None) -> None:
+    """star_attn_qk_norm_rope: queries Q and keys K [B, T, H, d] (either may be None) normed per head and rotated into
+    Yq and Yk (which may be Q and K)."""
+    tokens = (Q if Q is not None else K).shape[1]
+    _check(_calls().qk_norm_rope(shape, rotary.of(shape, tokens), tokens, Q, K, Yq, Yk, _stream(stream)))
+
+
+def phase1_norm_rope(shape: StarShape, rotary: Rotary, Q, K, V, O_ctx, K_cache, V_cache, LSE_ctx=None, workspace=None,
+                     stream=None) -> None:
+    """star_attn_phase1_norm_rope: phase 1 on queries (normed and rotated in place) and keys as they are projected."""
+    _check(_calls().phase1_norm_rope(shape, rotary.of(shape, shape.ctx_len), Q, K, V, O_ctx, LSE_ctx, K_cache, V_cache, workspace, _stream(stream)))
+
+
+def phase2_norm_rope(shape: StarShape, rotary: Rotary, cache_len: int, Qq, Kq, Vq, K_cache, V_cache, O, workspace,
+                     O_part=None, LSE_part=None, stream=None) -> None:
+    """star_attn_phase2_norm_rope: phase 2 on queries (normed and rotated in place) and keys as they are projected."""
+    _check(_calls().phase2_norm_rope(shape, rotary.of(shape, Qq.shape[1]), int(cache_len), Qq, Kq, Vq, K_cache, V_cache, O_part, LSE_part, O,
+                                     workspace, _stream(stream)))
+
+
+def alloc_q4_cache(shape: StarShape, device="cuda") -> Q4Cache:
+    """A caller-owned cache in four bits, all zeros."""
+    rows = (shape.batch, shape.n_kv_heads, shape.cache_capacity)
+    return Q4Cache(shape, *(torch.zeros(rows + (shape.head_dim // n,), dtype=torch.uint8, device=device) for n in (2, 32) * 2))
+
+
+def q4_workspace_bytes(shape: StarShape, max_q_len: int) -> int:
+    return int(load_library().star_attn_q4_workspace_bytes(ctypes.byref(shape), int(max_q_len)))
+
+
+def alloc_q4_workspace(shape: StarShape, max_q_len: int, device="cuda") -> torch.Tensor:
+    n = q4_workspace_bytes(shape, max_q_len)
+    if n == 0:
+        raise StarAttnError(-1, "invalid shape for workspace query")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def q4_store(shape: StarShape, first_row: int, n_rows: int, K, V, cache: Q4Cache, plain_row=None, stream=None) -> None:
+    """star_attn_q4_store: rows [plain_row, plain_row + n_rows) of K and V [B, Hkv, rows, d] (by default those of the same
+    numbers) into rows [first_row, first_row + n_rows) of the cache."""
+    _check(_calls().q4_store(shape, int(first_row), int(n_rows), K, V, int(first_row if plain_row is None else plain_row), cache.of(shape),
+                             _stream(stream)))
+
+
+def q4_load(shape: StarShape, first_row: int, n_rows: int, cache: Q4Cache, K, V, plain_row=None, stream=None) -> None:
+    """star_attn_q4_load: the same rows of the cache into K and V, as what their codes stand for."""
+    _check(_calls().q4_load(shape, int(first_row), int(n_rows), K, V, int(first_row if plain_row is None else plain_row), cache.of(shape),
+                            _stream(stream)))
+
+
+def phase2_q4(shape: StarShape, cache_len: int, Qq, Kq, Vq, cache: Q4Cache, O, workspace, rotary: Optional[Rotary] = None,
+              O_part=None, LSE_part=None, stream=None) -> None:
+    """star_attn_phase2_q4: files Kq/Vq in the four-bit cache at cache_len, then attends to all it holds; with `rotary`, Qq
+    (in place) and Kq are normed and rotated first."""
+    _check(_calls().phase2_q4(shape, None if rotary is None else rotary.of(shape, Qq.shape[1]), int(cache_len), Qq, Kq, Vq, cache.of(shape), O_part, LSE_part, O,
+                              workspace, _stream(stream)))
+
+
+def phase2_q4_partial(shape: StarShape, cache_len: int, Qq, cache: Q4Cache, A, LSE, workspace, Kq=None, Vq=None, stream=None) -> None:
+    """star_attn_phase2_q4_partial: one host's pair (A, LSE) over a four-bit cache (see phase2_partial)."""
+    _check(_calls().phase2_q4_partial(shape, int(cache_len), Qq, Kq, Vq, cache.of(shape), A, LSE, workspace, _stream(stream)))
+
+
+def phase2_q4_plan(shape: StarShape, cache_len: int, q_len: int, want_parts: bool = False) -> PlanInfo:
+    """star_attn_phase2_q4_plan: what a phase2_q4 call with these arguments would run."""
+    info = PlanInfo()
+    _check(load_library().star_attn_phase2_q4_plan(ctypes.byref(shape), int(cache_len), int(q_len), int(bool(want_parts)),
+                                                   ctypes.byref(info)))
+    return info

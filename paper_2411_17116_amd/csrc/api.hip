@@ -447,6 +447,39 @@ static bool make_plan(const star_attn_shape* s, int64_t q_len, int64_t total, bo
   return true;
 }
 
+// ---- four-bit cache: workgroups of 16 rows and a split, two of them on a CU.
+constexpr int64_t Q4_WGS = 512;
+constexpr int64_t Q4_SPLIT_MIN = 128;      // keys: a unit of 32 for each of four wavefronts
+static int64_t q4_splits(const Geom& g, int64_t q_len) {
+  const int64_t wgs = (int64_t)g.B * g.Hkv * ceil_div((int64_t)g.G * q_len, Q4_TILE);
+  return wgs < Q4_WGS ? Q4_WGS / wgs : 1;
+}
+static bool make_q4_plan(const Geom& g, int64_t q_len, int64_t total, bool want_parts, SplitPlan* p) {
+  *p = SplitPlan{};
+  const int64_t n = ceil_div(g.L, g.b), want = q4_splits(g, q_len);
+  p->tile_rows = Q4_TILE;
+  p->n_blocks = (int32_t)n;
+  if (n > (1 << 24)) return false;
+  if (!want_parts) {
+    const int64_t worth = ceil_div(total, Q4_SPLIT_MIN), splits = want < worth ? want : worth;
+    p->flat = 1;
+    p->split_len = round_up(ceil_div(total, splits), 32);
+    p->s_total = (int32_t)ceil_div(total, p->split_len);
+    return true;
+  }
+  const int64_t bmax = g.b < g.L ? g.b : g.L, most = bmax / Q4_SPLIT_MIN > 1 ? bmax / Q4_SPLIT_MIN : 1;
+  int64_t spb = ceil_div(want, n);
+  if (spb > most) spb = most;
+  p->split_len = round_up(ceil_div(bmax, spb), 32);
+  spb = ceil_div(bmax, p->split_len);
+  const int64_t st = g.cap > g.L ? ceil_div(g.cap - g.L, p->split_len) : 1;
+  if (n * spb + st > (1 << 24)) return false;
+  p->spb = (int32_t)spb;
+  p->st = (int32_t)st;
+  p->s_total = (int32_t)(n * spb + st);
+  return true;
+}
+
 static size_t plan_bytes(const star_attn_shape* s, const SplitPlan& p, int64_t q_len) {
   size_t rows = (size_t)s->batch * (size_t)p.s_total * (size_t)s->n_q_heads * (size_t)q_len;
   size_t bytes = rows * (size_t)(s->head_dim + 1) * sizeof(float);
@@ -459,6 +492,7 @@ static bool misaligned(const void* p) { return ((uintptr_t)p & 15u) != 0; }
 struct Rope {
   double theta;
   int64_t pos0;
+  const star_attn_rotary* more;      // of the *_norm_rope ones: norms and axes; else null
 };
 
 static int validate_rope(const star_attn_shape* s, double theta, int64_t pos0) {
@@ -466,6 +500,34 @@ static int validate_rope(const star_attn_shape* s, double theta, int64_t pos0) {
     return STAR_ATTN_ERR_INVALID_SHAPE;
   (void)s;    // every supported head_dim is even
   return STAR_ATTN_OK;
+}
+
+static int validate_rotary(const star_attn_shape* s, const star_attn_rotary* r) {
+  if (!r) return STAR_ATTN_ERR_NULL_POINTER;
+  int rc = validate_rope(s, r->rope_theta, r->pos0);
+  if (rc != STAR_ATTN_OK) return rc;
+  if (!(r->norm_eps >= 0.f) || isinf(r->norm_eps) || r->n_axes < 1 || r->n_axes > 4) return STAR_ATTN_ERR_INVALID_SHAPE;
+  for (int i = 0; i < s->head_dim / 2; ++i)
+    if (r->axis[i] >= r->n_axes) return STAR_ATTN_ERR_INVALID_SHAPE;
+  if (misaligned(r->positions) || misaligned(r->q_norm) || misaligned(r->k_norm)) return STAR_ATTN_ERR_MISALIGNED;
+  return STAR_ATTN_OK;
+}
+// What every launch_qk call takes from it; `pos0` of its first token.
+static QkArgs qk_args(const star_attn_rotary& r, int64_t n_tokens, int64_t pos0) {
+  QkArgs q = {};
+  q.n_tokens = n_tokens; q.theta = r.rope_theta; q.pos0 = pos0; q.positions = r.positions; q.n_axes = r.n_axes;
+  for (int i = 0; i < 64; ++i) q.axis[i >> 5] |= (uint64_t)(r.axis[i] & 3) << (2 * (i & 31));
+  q.q_norm = r.q_norm; q.k_norm = r.k_norm; q.eps = r.norm_eps;
+  return q;
+}
+// Queries rotated in place, keys and values into the caches, by either kind of rotation; `pos0` of the first token.
+static hipError_t rotate_call(const star_attn_shape* s, const Geom& g, const Rope& rope, void* Q, const void* K, const void* V, void* Kc,
+                              void* Vc, int64_t n_tokens, int64_t dst_row, int64_t pos0, unsigned int* clear, hipStream_t st) {
+  if (!rope.more) return launch_rope(s->dtype, g, g.Hq, Q, Q, K, V, Kc, Vc, n_tokens, dst_row, pos0, rope.theta, clear, st);
+  QkArgs q = qk_args(*rope.more, n_tokens, pos0);
+  q.Q = Q; q.Yq = Q; q.K = K; q.Yk = Kc; q.V = V; q.Vc = Vc;
+  q.cached = 1; q.dst_row = dst_row; q.clear = clear;
+  return launch_qk(s->dtype, g, q, st);
 }
 
 // Bytes of the separately given anchors (K or V), 256-byte padded.
@@ -578,7 +640,7 @@ static int phase1_impl(const star_attn_shape* shape, int anchor_mode, const Rope
                        size_t workspace_bytes, void* hip_stream) {
   int rc = validate_shape(shape);
   if (rc != STAR_ATTN_OK) return rc;
-  if (rope && (rc = validate_rope(shape, rope->theta, rope->pos0)) != STAR_ATTN_OK) return rc;
+  if (rope && (rc = rope->more ? validate_rotary(shape, rope->more) : validate_rope(shape, rope->theta, rope->pos0)) != STAR_ATTN_OK) return rc;
   if (!known_mode(anchor_mode)) return STAR_ATTN_ERR_INVALID_MODE;
   if (!Q || !K || !V || !O_ctx || !K_cache || !V_cache) return STAR_ATTN_ERR_NULL_POINTER;
   if (misaligned(Q) || misaligned(K) || misaligned(V) || misaligned(O_ctx) ||
@@ -638,8 +700,7 @@ static int phase1_impl(const star_attn_shape* shape, int anchor_mode, const Rope
   // Algorithm 1: keep the K/V of every block once (anchor copies never exist here).
   // The attention kernels read plain inputs where they are and file them in the
   // caches themselves; rotated keys go through the caches.
-  if (rope && launch_rope(shape->dtype, g, g.Hq, Q, Q, K, V, K_cache, V_cache, g.L, 0, rope->pos0, rope->theta,
-                          tickets, st) != hipSuccess)
+  if (rope && rotate_call(shape, g, *rope, Q, K, V, K_cache, V_cache, g.L, 0, rope->pos0, tickets, st) != hipSuccess)
     return STAR_ATTN_ERR_LAUNCH_FAILED;
   Phase1Args a;
   a.g = g; a.Q = Q; a.O = O_ctx; a.LSE = LSE_ctx; a.Kc = K_cache; a.Vc = V_cache;
@@ -676,7 +737,7 @@ int star_attn_phase1_rope(const star_attn_shape* shape, double rope_theta, int64
                           const void* K, const void* V, void* O_ctx, float* LSE_ctx,
                           void* K_cache, void* V_cache, void* workspace, size_t workspace_bytes,
                           void* hip_stream) {
-  Rope rope = {rope_theta, pos0};
+  Rope rope = {rope_theta, pos0, nullptr};
   return phase1_impl(shape, STAR_ATTN_ANCHOR_FIRST, &rope, Q, K, V, nullptr, nullptr, O_ctx,
                      LSE_ctx, K_cache, V_cache, workspace, workspace_bytes, hip_stream);
 }
@@ -708,7 +769,7 @@ static int phase2_impl(const star_attn_shape* shape, const Rope* rope, int64_t c
                        bool static_scratch = false) {
   int rc = validate_shape(shape);
   if (rc != STAR_ATTN_OK) return rc;
-  if (rope && (rc = validate_rope(shape, rope->theta, rope->pos0)) != STAR_ATTN_OK) return rc;
+  if (rope && (rc = rope->more ? validate_rotary(shape, rope->more) : validate_rope(shape, rope->theta, rope->pos0)) != STAR_ATTN_OK) return rc;
   if (q_len <= 0 || q_len > (1 << 20) || cache_len < shape->ctx_len) return STAR_ATTN_ERR_INVALID_SHAPE;
   const bool append = !(pair && !Kq && !Vq);
   const int64_t total = cache_len + (append ? q_len : 0);
@@ -751,13 +812,12 @@ static int phase2_impl(const star_attn_shape* shape, const Rope* rope, int64_t c
   // stored over Qq, which one launch would both merge into and rotate, nor where Kq are rows of the cache, which
   // would be read behind their rotation.)
   const size_t q_bytes = (size_t)g.B * q_len * g.Hq * g.d * 2, k_bytes = (size_t)g.B * q_len * g.Hkv * g.d * 2;
-  const bool turn = append && rope && plan.decode && plan.flat && g.G * q_len <= 16 && q_len <= DECODE_ROPE_TOKENS &&
+  const bool turn = append && rope && !rope->more && plan.decode && plan.flat && g.G * q_len <= 16 && q_len <= DECODE_ROPE_TOKENS &&
                     (int64_t)g.B * g.Hq * q_len <= (1 << 20) && !overlap(O, q_bytes, Qq, q_bytes) &&
                     !overlap(Kq, k_bytes, K_cache, (size_t)g.B * g.Hkv * g.cap * g.d * 2);
   const bool fused_append = append && (!rope || turn);
   if (append && rope && !turn &&
-      launch_rope(shape->dtype, g, g.Hq, Qq, Qq, Kq, Vq, K_cache, V_cache, q_len, cache_len,
-                  rope->pos0 + cache_len, rope->theta, nullptr, st) != hipSuccess)
+      rotate_call(shape, g, *rope, Qq, Kq, Vq, K_cache, V_cache, q_len, cache_len, rope->pos0 + cache_len, nullptr, st) != hipSuccess)
     return STAR_ATTN_ERR_LAUNCH_FAILED;
 
   size_t rows = (size_t)g.B * plan.s_total * g.Hq * (size_t)q_len;
@@ -789,6 +849,7 @@ static int phase2_impl(const star_attn_shape* shape, const Rope* rope, int64_t c
   // 23 on 2048 (32 / 8 heads) 20.2 / 16.2.  The sums are held in 64 bits, as merge part by part compensates its own (in
   // 32 bits: 18.3, 18.4, 18.1, 14.4, 15.7).  (The kernels of one part number a row's pieces in one launch.)
   m.wide = 0;
+  m.keep_nan = 0;
   if (!O_part && !plan.flat && (int64_t)g.B * g.Hq * q_len < (1 << 22)) { m.plan.flat = 1; m.wide = 1; }
   m.q_len = (int32_t)q_len; m.out_bf16 = shape->dtype == STAR_ATTN_BF16;
   m.O_sub = a.O_sub; m.LSE_sub = a.LSE_sub; m.O_part = O_part; m.LSE_part = LSE_part;
@@ -855,7 +916,7 @@ int star_attn_merge(const star_attn_shape* shape, int64_t n_parts, int64_t q_len
   m.split_stride = rows;
   m.O_part = nullptr; m.LSE_part = nullptr;
   m.O = O; m.A = A; m.LSE = LSE;
-  m.Qq = nullptr; m.rotary = Rotary{0.0, 0}; m.wide = 0;
+  m.Qq = nullptr; m.rotary = Rotary{0.0, 0}; m.wide = 0; m.keep_nan = 0;
   return launch_merge(m, (hipStream_t)hip_stream) == hipSuccess ? STAR_ATTN_OK
                                                                 : STAR_ATTN_ERR_LAUNCH_FAILED;
 }
@@ -865,9 +926,196 @@ int star_attn_phase2_rope(const star_attn_shape* shape, double rope_theta, int64
                           const void* Vq, void* K_cache, void* V_cache, float* O_part,
                           float* LSE_part, void* O, void* workspace, size_t workspace_bytes,
                           void* hip_stream) {
-  Rope rope = {rope_theta, pos0};
+  Rope rope = {rope_theta, pos0, nullptr};
   return phase2_impl(shape, &rope, cache_len, q_len, Qq, Kq, Vq, K_cache, V_cache, O_part,
                      LSE_part, O, false, nullptr, nullptr, workspace, workspace_bytes, hip_stream);
+}
+
+int star_attn_qk_norm_rope(const star_attn_shape* shape, const star_attn_rotary* rotary, int64_t n_tokens,
+                           const void* Q, const void* K, void* Yq, void* Yk, void* hip_stream) {
+  int rc = validate_shape(shape);
+  if (rc != STAR_ATTN_OK) return rc;
+  if ((rc = validate_rotary(shape, rotary)) != STAR_ATTN_OK) return rc;
+  if (n_tokens <= 0 || (int64_t)shape->batch * n_tokens > 0x7fffffff) return STAR_ATTN_ERR_INVALID_SHAPE;
+  if ((!Q && !K) || !Q != !Yq || !K != !Yk) return STAR_ATTN_ERR_NULL_POINTER;
+  if (misaligned(Q) || misaligned(K) || misaligned(Yq) || misaligned(Yk)) return STAR_ATTN_ERR_MISALIGNED;
+  QkArgs q = qk_args(*rotary, n_tokens, rotary->pos0);
+  q.Q = Q; q.K = K; q.Yq = Yq; q.Yk = Yk;
+  return launch_qk(shape->dtype, make_geom(shape), q, (hipStream_t)hip_stream) == hipSuccess ? STAR_ATTN_OK : STAR_ATTN_ERR_LAUNCH_FAILED;
+}
+
+int star_attn_phase1_norm_rope(const star_attn_shape* shape, const star_attn_rotary* rotary, void* Q,
+                               const void* K, const void* V, void* O_ctx, float* LSE_ctx,
+                               void* K_cache, void* V_cache, void* workspace, size_t workspace_bytes,
+                               void* hip_stream) {
+  if (!rotary) return shape ? STAR_ATTN_ERR_NULL_POINTER : validate_shape(shape);
+  Rope rope = {rotary->rope_theta, rotary->pos0, rotary};
+  return phase1_impl(shape, STAR_ATTN_ANCHOR_FIRST, &rope, Q, K, V, nullptr, nullptr, O_ctx,
+                     LSE_ctx, K_cache, V_cache, workspace, workspace_bytes, hip_stream);
+}
+
+int star_attn_phase2_norm_rope(const star_attn_shape* shape, const star_attn_rotary* rotary,
+                               int64_t cache_len, int64_t q_len, void* Qq, const void* Kq,
+                               const void* Vq, void* K_cache, void* V_cache, float* O_part,
+                               float* LSE_part, void* O, void* workspace, size_t workspace_bytes,
+                               void* hip_stream) {
+  if (!rotary) return STAR_ATTN_ERR_NULL_POINTER;
+  Rope rope = {rotary->rope_theta, rotary->pos0, rotary};
+  return phase2_impl(shape, &rope, cache_len, q_len, Qq, Kq, Vq, K_cache, V_cache, O_part,
+                     LSE_part, O, false, nullptr, nullptr, workspace, workspace_bytes, hip_stream);
+}
+
+}  // extern "C"
+
+static int validate_q4(const star_attn_q4_cache* c) {
+  if (!c || !c->k_codes || !c->k_scales || !c->v_codes || !c->v_scales) return STAR_ATTN_ERR_NULL_POINTER;
+  if (misaligned(c->k_codes) || misaligned(c->k_scales) || misaligned(c->v_codes) || misaligned(c->v_scales))
+    return STAR_ATTN_ERR_MISALIGNED;
+  return STAR_ATTN_OK;
+}
+
+static int q4_copy(const star_attn_shape* shape, int64_t first_row, int64_t n_rows, const star_attn_q4_cache* cache, void* K, void* V,
+                   int64_t plain_rows, int64_t plain_row, void* hip_stream, bool load) {
+  int rc = validate_shape(shape);
+  if (rc != STAR_ATTN_OK) return rc;
+  if (first_row < 0 || n_rows <= 0 || plain_row < 0 || plain_rows <= 0) return STAR_ATTN_ERR_INVALID_SHAPE;
+  if (n_rows > shape->cache_capacity || first_row > shape->cache_capacity - n_rows || n_rows > plain_rows || plain_row > plain_rows - n_rows)
+    return STAR_ATTN_ERR_CACHE_OVERFLOW;
+  const Geom g = make_geom(shape);
+  if ((int64_t)g.B * g.Hkv * n_rows > 0x7fffffff || plain_rows > 0x7ff00000) return STAR_ATTN_ERR_INVALID_SHAPE;
+  if (!K || !V) return STAR_ATTN_ERR_NULL_POINTER;
+  if ((rc = validate_q4(cache)) != STAR_ATTN_OK) return rc;
+  if (misaligned(K) || misaligned(V)) return STAR_ATTN_ERR_MISALIGNED;
+  const size_t skip = (size_t)plain_row * g.d * (shape->dtype == STAR_ATTN_F32 ? 4 : 2);
+  const Q4Copy c = {{cache->k_codes, cache->k_scales, cache->v_codes, cache->v_scales}, (char*)K + skip, (char*)V + skip,
+                    g.Hkv * plain_rows * g.d, plain_rows * g.d, g.d, first_row, n_rows};
+  const hipError_t e = load ? launch_q4_load(shape->dtype, g, c, (hipStream_t)hip_stream) : launch_q4_store(shape->dtype, g, c, (hipStream_t)hip_stream);
+  return e == hipSuccess ? STAR_ATTN_OK : STAR_ATTN_ERR_LAUNCH_FAILED;
+}
+
+// Phase 2 over a four-bit cache, behind both public variants; `pair` as in phase2_impl.
+static int phase2_q4_impl(const star_attn_shape* shape, const star_attn_rotary* rotary, int64_t cache_len, int64_t q_len, void* Qq,
+                          const void* Kq, const void* Vq, const star_attn_q4_cache* cache, float* O_part, float* LSE_part, void* O,
+                          bool pair, float* A, float* LSE, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  int rc = validate_shape(shape);
+  if (rc != STAR_ATTN_OK) return rc;
+  if (rotary && (rc = validate_rotary(shape, rotary)) != STAR_ATTN_OK) return rc;
+  if (q_len <= 0 || q_len > (1 << 20) || cache_len < shape->ctx_len) return STAR_ATTN_ERR_INVALID_SHAPE;
+  const bool append = !(pair && !Kq && !Vq);
+  const int64_t total = cache_len + (append ? q_len : 0);
+  if (total > shape->cache_capacity) return STAR_ATTN_ERR_CACHE_OVERFLOW;
+  if (!Qq || !workspace || (append && (!Kq || !Vq)) || (pair ? (!A || !LSE) : !O) || (O_part == nullptr) != (LSE_part == nullptr))
+    return STAR_ATTN_ERR_NULL_POINTER;
+  if ((rc = validate_q4(cache)) != STAR_ATTN_OK) return rc;
+  if (misaligned(Qq) || misaligned(Kq) || misaligned(Vq) || misaligned(O) || misaligned(O_part) || ((uintptr_t)LSE_part & 3u) ||
+      misaligned(A) || ((uintptr_t)LSE & 3u) || ((uintptr_t)workspace & 255u))
+    return STAR_ATTN_ERR_MISALIGNED;
+  const Geom g = make_geom(shape);
+  SplitPlan plan;
+  if (!make_q4_plan(g, q_len, total, O_part != nullptr, &plan)) return STAR_ATTN_ERR_INVALID_SHAPE;
+  if (workspace_bytes < plan_bytes(shape, plan, q_len)) return STAR_ATTN_ERR_WORKSPACE_TOO_SMALL;
+  const int64_t rows = (int64_t)g.B * g.Hq * q_len;
+  if (rows * plan.s_total > 0x7fffffff) return STAR_ATTN_ERR_INVALID_SHAPE;
+  hipStream_t st = (hipStream_t)hip_stream;
+  const Q4Rows q4 = {cache->k_codes, cache->k_scales, cache->v_codes, cache->v_scales};
+
+  // Algorithm 2: the new tokens join the cache before they attend
+  if (append) {
+    hipError_t e;
+    if (rotary) {
+      QkArgs q = qk_args(*rotary, q_len, rotary->pos0 + cache_len);
+      q.Q = Qq; q.Yq = Qq; q.K = Kq; q.V = Vq; q.q4 = q4; q.dst_row = cache_len;
+      e = launch_qk(shape->dtype, g, q, st);
+    } else {
+      const Q4Copy c = {q4, const_cast<void*>(Kq), const_cast<void*>(Vq), q_len * g.Hkv * g.d, g.d, (int64_t)g.Hkv * g.d, cache_len, q_len};
+      e = launch_q4_store(shape->dtype, g, c, st);
+    }
+    if (e != hipSuccess) return STAR_ATTN_ERR_LAUNCH_FAILED;
+  }
+  Q4Args a;
+  a.g = g; a.plan = plan; a.cache_len = cache_len; a.q_len = (int32_t)q_len; a.causal = append ? 1 : 0;
+  a.parts = pair || O_part ? 2 : 1;        // (weights in bf16 are what bf16 outputs show; fp32 ones are held to more)
+  a.Qq = Qq; a.q4 = q4;
+  a.O_sub = (float*)workspace;
+  a.LSE_sub = (float*)workspace + rows * plan.s_total * g.d;
+  if (launch_phase2_q4(shape->dtype, a, st) != hipSuccess) return STAR_ATTN_ERR_LAUNCH_FAILED;
+  MergeArgs m;
+  m.g = g; m.plan = plan; m.wide = 0; m.keep_nan = 1;
+  m.q_len = (int32_t)q_len; m.out_bf16 = shape->dtype == STAR_ATTN_BF16;
+  m.O_sub = a.O_sub; m.LSE_sub = a.LSE_sub; m.O_part = O_part; m.LSE_part = LSE_part;
+  m.batch_stride = (int64_t)plan.s_total * g.Hq * q_len;
+  m.split_stride = (int64_t)g.Hq * q_len;
+  m.O = pair ? nullptr : O;
+  m.A = pair ? A : nullptr;
+  m.LSE = pair ? LSE : nullptr;
+  m.Qq = nullptr; m.rotary = Rotary{0.0, 0};
+  return launch_merge(m, st) == hipSuccess ? STAR_ATTN_OK : STAR_ATTN_ERR_LAUNCH_FAILED;
+}
+
+extern "C" {
+
+int star_attn_q4_store(const star_attn_shape* shape, int64_t first_row, int64_t n_rows, const void* K, const void* V,
+                       int64_t plain_rows, int64_t plain_row, const star_attn_q4_cache* cache, void* hip_stream) {
+  return q4_copy(shape, first_row, n_rows, cache, const_cast<void*>(K), const_cast<void*>(V), plain_rows, plain_row, hip_stream, false);
+}
+
+int star_attn_q4_load(const star_attn_shape* shape, int64_t first_row, int64_t n_rows, const star_attn_q4_cache* cache,
+                      void* K, void* V, int64_t plain_rows, int64_t plain_row, void* hip_stream) {
+  return q4_copy(shape, first_row, n_rows, cache, K, V, plain_rows, plain_row, hip_stream, true);
+}
+
+size_t star_attn_q4_workspace_bytes(const star_attn_shape* shape, int64_t max_q_len) {
+  if (validate_shape(shape) != STAR_ATTN_OK || max_q_len <= 0) return 0;
+  const Geom g = make_geom(shape);
+  size_t best = 0;
+  // A call's splits go by how many the resident workgroups leave for its rows, and by the cache: the longest call of each such number.
+  auto consider = [&](int64_t q) {
+    SplitPlan p;
+    if (make_q4_plan(g, q, g.cap, true, &p) && plan_bytes(shape, p, q) > best) best = plan_bytes(shape, p, q);
+    // (equal runs of a shorter cache may be more than the whole cache's, whose length is rounded up)
+    const int64_t want = q4_splits(g, q), worth = ceil_div(g.cap, Q4_SPLIT_MIN);
+    p.s_total = (int32_t)(want < worth ? want : worth);
+    if (plan_bytes(shape, p, q) > best) best = plan_bytes(shape, p, q);
+  };
+  const int64_t pairs = (int64_t)g.B * g.Hkv;
+  for (int64_t want = 1; want * pairs <= Q4_WGS; ++want) {
+    const int64_t q = Q4_WGS / (pairs * want) * Q4_TILE / g.G;
+    if (q >= 1) consider(q < max_q_len ? q : max_q_len);
+  }
+  consider(max_q_len);
+  return best;
+}
+
+int star_attn_phase2_q4(const star_attn_shape* shape, const star_attn_rotary* rotary, int64_t cache_len, int64_t q_len,
+                        void* Qq, const void* Kq, const void* Vq, const star_attn_q4_cache* cache, float* O_part,
+                        float* LSE_part, void* O, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  return phase2_q4_impl(shape, rotary, cache_len, q_len, Qq, Kq, Vq, cache, O_part, LSE_part, O, false, nullptr, nullptr, workspace,
+                        workspace_bytes, hip_stream);
+}
+
+int star_attn_phase2_q4_partial(const star_attn_shape* shape, int64_t cache_len, int64_t q_len, const void* Qq, const void* Kq,
+                                const void* Vq, const star_attn_q4_cache* cache, float* A, float* LSE, void* workspace,
+                                size_t workspace_bytes, void* hip_stream) {
+  if ((Kq == nullptr) != (Vq == nullptr)) return STAR_ATTN_ERR_NULL_POINTER;
+  return phase2_q4_impl(shape, nullptr, cache_len, q_len, const_cast<void*>(Qq), Kq, Vq, cache, nullptr, nullptr, nullptr, true, A, LSE,
+                        workspace, workspace_bytes, hip_stream);
+}
+
+int star_attn_phase2_q4_plan(const star_attn_shape* shape, int64_t cache_len, int64_t q_len, int want_parts, star_attn_plan_info* out) {
+  int rc = validate_shape(shape);
+  if (rc != STAR_ATTN_OK) return rc;
+  if (!out) return STAR_ATTN_ERR_NULL_POINTER;
+  if (q_len <= 0 || q_len > (1 << 20) || cache_len < shape->ctx_len) return STAR_ATTN_ERR_INVALID_SHAPE;
+  if (cache_len + q_len > shape->cache_capacity) return STAR_ATTN_ERR_CACHE_OVERFLOW;
+  SplitPlan plan;
+  if (!make_q4_plan(make_geom(shape), q_len, cache_len + q_len, want_parts != 0, &plan)) return STAR_ATTN_ERR_INVALID_SHAPE;
+  *out = star_attn_plan_info{};
+  out->flat = plan.flat;
+  out->n_splits = plan.s_total;
+  out->tile_rows = plan.tile_rows;
+  out->split_len = plan.split_len;
+  out->workspace_bytes = (int64_t)plan_bytes(shape, plan, q_len);
+  return STAR_ATTN_OK;
 }
 
 const char* star_attn_status_string(int status) {

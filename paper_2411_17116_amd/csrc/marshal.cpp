@@ -30,6 +30,16 @@ struct EntryPoints {
   decltype(&star_attn_merge) merge;
   decltype(&star_attn_rope) rope;
 } lib;
+// Those around a cache in four bits, by position in bind_q4()'s.
+struct Q4EntryPoints {
+  decltype(&star_attn_qk_norm_rope) qk_norm_rope;
+  decltype(&star_attn_phase1_norm_rope) phase1_norm_rope;
+  decltype(&star_attn_phase2_norm_rope) phase2_norm_rope;
+  decltype(&star_attn_q4_store) q4_store;
+  decltype(&star_attn_q4_load) q4_load;
+  decltype(&star_attn_phase2_q4) phase2_q4;
+  decltype(&star_attn_phase2_q4_partial) phase2_q4_partial;
+} q4lib;
 
 // Reads a call's arguments in order; `ok` is false once a Python error is set.
 struct Args {
@@ -38,12 +48,15 @@ struct Args {
   bool ok = true;
   Py_buffer view;
   bool has_view = false;
+  Py_buffer records[2];
+  int n_records = 0;
 
   Args(PyObject* const* args, Py_ssize_t n, Py_ssize_t want) : at(args), end(args + n) {
     if (n != want) fail(PyExc_TypeError, "wrong number of arguments");
   }
   ~Args() {
     if (has_view) PyBuffer_Release(&view);
+    while (n_records > 0) PyBuffer_Release(&records[--n_records]);
   }
   void fail(PyObject* type, const char* what) {
     if (ok) PyErr_SetString(type, what);
@@ -63,6 +76,23 @@ struct Args {
     if (view.len < (Py_ssize_t)sizeof(star_attn_shape)) { fail(PyExc_TypeError, "a StarShape is wanted"); return nullptr; }
     return (const star_attn_shape*)view.buf;
   }
+  // A ctypes struct that mirrors Record, or None.
+  template <typename Record>
+  const Record* record(const char* what) {
+    PyObject* o = next();
+    if (!o || o == Py_None) return nullptr;
+    Py_buffer* v = &records[n_records];
+    if (n_records >= 2 || PyObject_GetBuffer(o, v, PyBUF_SIMPLE) != 0) {
+      PyErr_Clear();
+      fail(PyExc_TypeError, what);
+      return nullptr;
+    }
+    ++n_records;
+    if (v->len != (Py_ssize_t)sizeof(Record)) { fail(PyExc_TypeError, what); return nullptr; }
+    return (const Record*)v->buf;
+  }
+  const star_attn_rotary* rotary() { return record<star_attn_rotary>("a Rotary is wanted"); }
+  const star_attn_q4_cache* q4() { return record<star_attn_q4_cache>("a Q4Cache is wanted"); }
   int64_t integer() {
     PyObject* o = next();
     if (!o) return 0;
@@ -271,35 +301,129 @@ FASTCALL(rope) {
   return finish(a, (const void*)lib.rope, [&] { return lib.rope(s, (int32_t)heads, tokens, pos0, theta, X, Y, st); });
 }
 
-// bind(StarShape, (addresses of the entry points, in the order of EntryPoints))
-PyObject* bind(PyObject*, PyObject* args) {
-  PyObject *type, *addresses;
-  if (!PyArg_ParseTuple(args, "O!O!", &PyType_Type, &type, &PyTuple_Type, &addresses)) return nullptr;
-  void* p[sizeof(EntryPoints) / sizeof(void*)];
+// qk_norm_rope(shape, rotary, n_tokens, Q, K, Yq, Yk, stream)
+FASTCALL(qk_norm_rope) {
+  Args a(args, n, 8);
+  const star_attn_shape* s = a.shape();
+  const star_attn_rotary* r = a.rotary();
+  const int64_t tokens = a.integer();
+  void *Q = a.pointer(), *K = a.pointer(), *Yq = a.pointer(), *Yk = a.pointer(), *st = a.stream();
+  return finish(a, (const void*)q4lib.qk_norm_rope, [&] { return q4lib.qk_norm_rope(s, r, tokens, Q, K, Yq, Yk, st); });
+}
+// phase1_norm_rope(shape, rotary, Q, K, V, O_ctx, LSE_ctx, K_cache, V_cache, workspace, stream)
+FASTCALL(phase1_norm_rope) {
+  Args a(args, n, 11);
+  const star_attn_shape* s = a.shape();
+  const star_attn_rotary* r = a.rotary();
+  void *Q = a.pointer(), *K = a.pointer(), *V = a.pointer(), *O = a.pointer(), *L = a.pointer(), *Kc = a.pointer(), *Vc = a.pointer();
+  int64_t ws_n;
+  void *ws = a.sized(-1, &ws_n), *st = a.stream();
+  return finish(a, (const void*)q4lib.phase1_norm_rope,
+                [&] { return q4lib.phase1_norm_rope(s, r, Q, K, V, O, (float*)L, Kc, Vc, ws, (size_t)ws_n, st); });
+}
+// phase2_norm_rope(shape, rotary, cache_len, Qq, Kq, Vq, K_cache, V_cache, O_part, LSE_part, O, workspace, stream)
+FASTCALL(phase2_norm_rope) {
+  Args a(args, n, 13);
+  const star_attn_shape* s = a.shape();
+  const star_attn_rotary* r = a.rotary();
+  const int64_t cached = a.integer();
+  int64_t q, ws_n;
+  void *Q = a.sized(1, &q), *K = a.pointer(), *V = a.pointer(), *Kc = a.pointer(), *Vc = a.pointer(), *Op = a.pointer(),
+       *Lp = a.pointer(), *O = a.pointer(), *ws = a.sized(-1, &ws_n), *st = a.stream();
+  return finish(a, (const void*)q4lib.phase2_norm_rope, [&] {
+    return q4lib.phase2_norm_rope(s, r, cached, q, Q, K, V, Kc, Vc, (float*)Op, (float*)Lp, O, ws, (size_t)ws_n, st);
+  });
+}
+// q4_store(shape, first_row, n_rows, K, V, plain_row, cache, stream), K and V [B, Hkv, plain_rows, d]; q4_load the same
+template <typename Call>
+PyObject* q4_rows(Args& a, const void* entry, Call call) {
+  const star_attn_shape* s = a.shape();
+  const int64_t row = a.integer(), rows = a.integer();
+  int64_t plain_rows;
+  void *K = a.sized(2, &plain_rows), *V = a.pointer();
+  const int64_t plain_row = a.integer();
+  const star_attn_q4_cache* c = a.q4();
+  void* st = a.stream();
+  return finish(a, entry, [&] { return call(s, row, rows, K, V, plain_rows, plain_row, c, st); });
+}
+FASTCALL(q4_store) {
+  Args a(args, n, 8);
+  return q4_rows(a, (const void*)q4lib.q4_store, q4lib.q4_store);
+}
+FASTCALL(q4_load) {
+  Args a(args, n, 8);
+  return q4_rows(a, (const void*)q4lib.q4_load,
+                 [](const star_attn_shape* s, int64_t row, int64_t rows, void* K, void* V, int64_t plain_rows, int64_t plain_row,
+                    const star_attn_q4_cache* c, void* st) { return q4lib.q4_load(s, row, rows, c, K, V, plain_rows, plain_row, st); });
+}
+// phase2_q4(shape, rotary, cache_len, Qq, Kq, Vq, cache, O_part, LSE_part, O, workspace, stream)
+FASTCALL(phase2_q4) {
+  Args a(args, n, 12);
+  const star_attn_shape* s = a.shape();
+  const star_attn_rotary* r = a.rotary();
+  const int64_t cached = a.integer();
+  int64_t q, ws_n;
+  void *Q = a.sized(1, &q), *K = a.pointer(), *V = a.pointer();
+  const star_attn_q4_cache* c = a.q4();
+  void *Op = a.pointer(), *Lp = a.pointer(), *O = a.pointer(), *ws = a.sized(-1, &ws_n), *st = a.stream();
+  return finish(a, (const void*)q4lib.phase2_q4,
+                [&] { return q4lib.phase2_q4(s, r, cached, q, Q, K, V, c, (float*)Op, (float*)Lp, O, ws, (size_t)ws_n, st); });
+}
+// phase2_q4_partial(shape, cache_len, Qq, Kq, Vq, cache, A, LSE, workspace, stream)
+FASTCALL(phase2_q4_partial) {
+  Args a(args, n, 10);
+  const star_attn_shape* s = a.shape();
+  const int64_t cached = a.integer();
+  int64_t q, ws_n;
+  void *Q = a.sized(1, &q), *K = a.pointer(), *V = a.pointer();
+  const star_attn_q4_cache* c = a.q4();
+  void *A = a.pointer(), *L = a.pointer(), *ws = a.sized(-1, &ws_n), *st = a.stream();
+  return finish(a, (const void*)q4lib.phase2_q4_partial,
+                [&] { return q4lib.phase2_q4_partial(s, cached, q, Q, K, V, c, (float*)A, (float*)L, ws, (size_t)ws_n, st); });
+}
+
+// The addresses of a tuple into a struct of entry points.
+template <typename Points>
+bool read_addresses(PyObject* addresses, Points& to) {
+  void* p[sizeof(Points) / sizeof(void*)];
   constexpr Py_ssize_t n = sizeof(p) / sizeof(p[0]);
   if (PyTuple_GET_SIZE(addresses) != n) {
     PyErr_SetString(PyExc_ValueError, "wrong number of entry points");
-    return nullptr;
+    return false;
   }
   for (Py_ssize_t i = 0; i < n; ++i) {
     p[i] = PyLong_AsVoidPtr(PyTuple_GET_ITEM(addresses, i));
     if (!p[i]) {
       if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "null entry point");
-      return nullptr;
+      return false;
     }
   }
-  static_assert(sizeof(lib) == sizeof(p), "nothing but function pointers");
-  memcpy((void*)&lib, p, sizeof(lib));
+  static_assert(sizeof(to) == sizeof(p), "nothing but function pointers");
+  memcpy((void*)&to, p, sizeof(to));
+  return true;
+}
+// bind(StarShape, (addresses of the entry points, in the order of EntryPoints))
+PyObject* bind(PyObject*, PyObject* args) {
+  PyObject *type, *addresses;
+  if (!PyArg_ParseTuple(args, "O!O!", &PyType_Type, &type, &PyTuple_Type, &addresses) || !read_addresses(addresses, lib)) return nullptr;
   Py_INCREF(type);
   Py_XDECREF(shape_type);
   shape_type = type;
+  Py_RETURN_NONE;
+}
+// bind_q4((addresses in the order of Q4EntryPoints))
+PyObject* bind_q4(PyObject*, PyObject* args) {
+  PyObject* addresses;
+  if (!PyArg_ParseTuple(args, "O!", &PyTuple_Type, &addresses) || !read_addresses(addresses, q4lib)) return nullptr;
   Py_RETURN_NONE;
 }
 
 #define ENTRY(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {ENTRY(phase1), ENTRY(phase1_anchor), ENTRY(phase1_rope), ENTRY(phase2), ENTRY(phase2_rope),
                          ENTRY(phase2_static), ENTRY(phase2_partial), ENTRY(merge), ENTRY(rope),
-                         {"bind", bind, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
+                         ENTRY(qk_norm_rope), ENTRY(phase1_norm_rope), ENTRY(phase2_norm_rope), ENTRY(q4_store), ENTRY(q4_load),
+                         ENTRY(phase2_q4), ENTRY(phase2_q4_partial),
+                         {"bind", bind, METH_VARARGS, nullptr}, {"bind_q4", bind_q4, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", "libstarattn's entry points on torch tensors", -1, methods,
                       nullptr, nullptr, nullptr, nullptr};
 

@@ -39,6 +39,9 @@ namespace {
 
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 
+// Whether a sum of weights is of something: NaN, from a split whose log-sum-exp is, counts only if the call says so.
+__device__ __forceinline__ bool some(float w, int keep_nan) { return w > 0.f || (keep_nan && w != w); }
+
 // sum += x with the rounding error of the addition carried in `comp`
 __device__ __forceinline__ void add_compensated(float& sum, float& comp, float x) {
   const float y = x - comp;
@@ -139,16 +142,16 @@ __global__ __launch_bounds__(32 * GROUPS) void merge_kernel(MergeArgs a, unsigne
         float t = 0.f;
 #pragma unroll
         for (int k = 0; k < GROUPS; ++k) t += red_acc[k][li * E + e];
-        A_m[e] = wtot > 0.f ? t / wtot : 0.f;
+        A_m[e] = some(wtot, a.keep_nan) ? t / wtot : 0.f;
       }
-      if (wtot > 0.f) lse_m = pm + logf(wtot);
+      if (some(wtot, a.keep_nan)) lse_m = pm + logf(wtot);
       if (a.O_part) {
         int64_t pr = (((int64_t)beta * n_parts + m) * g.Hq + h) * a.q_len + j;
 #pragma unroll
         for (int e = 0; e < E; ++e) a.O_part[pr * D + li * E + e] = A_m[e];
         if (li == 0) a.LSE_part[pr] = lse_m;
       }
-      if (lse_m > -INFINITY) {
+      if (lse_m > -INFINITY || (a.keep_nan && lse_m != lse_m)) {
         float m_new = fmaxf(m_g, lse_m);
         float sc_old = expf(m_g - m_new);     // 0 on the first non-empty part
         float sc_new = expf(lse_m - m_new);
@@ -170,13 +173,13 @@ __global__ __launch_bounds__(32 * GROUPS) void merge_kernel(MergeArgs a, unsigne
     int64_t arow = ((int64_t)beta * g.Hq + h) * a.q_len + j;
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-      float out = l_g > 0.f ? acc_g[e] / l_g : 0.f;
+      float out = some(l_g, a.keep_nan) ? acc_g[e] / l_g : 0.f;
       if (a.A) a.A[arow * D + li * E + e] = out;
       if (!a.O) continue;
       if (a.out_bf16) ((unsigned short*)a.O)[orow * D + li * E + e] = f32_to_bf16_rne(out);
       else ((float*)a.O)[orow * D + li * E + e] = out;
     }
-    if (a.LSE && li == 0) a.LSE[arow] = l_g > 0.f ? m_g + logf(l_g) : -INFINITY;
+    if (a.LSE && li == 0) a.LSE[arow] = some(l_g, a.keep_nan) ? m_g + logf(l_g) : -INFINITY;
   }
 }
 
@@ -239,15 +242,15 @@ __global__ __launch_bounds__(256) void merge_rows_kernel(MergeArgs a, int64_t n_
     }
     float A_m[E];
 #pragma unroll
-    for (int e = 0; e < E; ++e) A_m[e] = wsum > 0.f ? acc[e] / wsum : 0.f;
-    const float lse_m = wsum > 0.f ? pm + logf(wsum) : -INFINITY;
+    for (int e = 0; e < E; ++e) A_m[e] = some(wsum, a.keep_nan) ? acc[e] / wsum : 0.f;
+    const float lse_m = some(wsum, a.keep_nan) ? pm + logf(wsum) : -INFINITY;
     if (a.O_part) {
       int64_t pr = (((int64_t)beta * n_parts + m) * g.Hq + h) * a.q_len + j;
 #pragma unroll
       for (int e = 0; e < E; ++e) a.O_part[pr * D + li * E + e] = A_m[e];
       if (li == 0) a.LSE_part[pr] = lse_m;
     }
-    if (lse_m > -INFINITY) {
+    if (lse_m > -INFINITY || (a.keep_nan && lse_m != lse_m)) {
       float m_new = fmaxf(m_g, lse_m);
       float sc_old = expf(m_g - m_new);          // 0 on the first non-empty part
       float sc_new = expf(lse_m - m_new);
@@ -267,13 +270,13 @@ __global__ __launch_bounds__(256) void merge_rows_kernel(MergeArgs a, int64_t n_
   const int64_t arow = ((int64_t)beta * g.Hq + h) * a.q_len + j;
 #pragma unroll
   for (int e = 0; e < E; ++e) {
-    float out = l_g > 0.f ? acc_g[e] / l_g : 0.f;
+    float out = some(l_g, a.keep_nan) ? acc_g[e] / l_g : 0.f;
     if (a.A) a.A[arow * D + li * E + e] = out;
     if (!a.O) continue;
     if (a.out_bf16) ((unsigned short*)a.O)[orow * D + li * E + e] = f32_to_bf16_rne(out);
     else ((float*)a.O)[orow * D + li * E + e] = out;
   }
-  if (a.LSE && li == 0) a.LSE[arow] = l_g > 0.f ? m_g + logf(l_g) : -INFINITY;
+  if (a.LSE && li == 0) a.LSE[arow] = some(l_g, a.keep_nan) ? m_g + logf(l_g) : -INFINITY;
 }
 
 // ------------------------------------------------------------------ one part
@@ -298,14 +301,15 @@ struct FlatMerge {
   float *A, *LSE;
   int64_t batch_stride, split_stride;
   int32_t Hq, q_len, S;
-  int16_t d, out_bf16;
+  int16_t d;
+  int8_t out_bf16, keep_nan;
   void* Qq;
   Rotary rotary;
 };
 static_assert(sizeof(FlatMerge) + 16 <= 112, "(and what merge_flat_rows_kernel takes besides)");
 inline FlatMerge pack(const MergeArgs& a) {
   return FlatMerge{a.O_sub, a.LSE_sub, a.O, a.A, a.LSE, a.batch_stride, a.split_stride, a.g.Hq, a.q_len, a.plan.s_total,
-                   (int16_t)a.g.d, (int16_t)a.out_bf16, a.Qq, a.rotary};
+                   (int16_t)a.g.d, (int8_t)a.out_bf16, (int8_t)a.keep_nan, a.Qq, a.rotary};
 }
 
 // What one lane gathers: the weighted sum of its four elements of the splits' outputs, the
@@ -351,7 +355,7 @@ __device__ __forceinline__ void fold_splits(Fold<Sum>& f, const float (&ls)[N], 
 }
 template <typename Sum>
 __device__ __forceinline__ void store_merged(const FlatMerge& a, int beta, int h, int64_t j, int d0, const Fold<Sum>& f) {
-  const f32x4 out = f.w > 0 ? __builtin_convertvector(f.acc / f.w, f32x4) : f32x4{0.f, 0.f, 0.f, 0.f};
+  const f32x4 out = some((float)f.w, a.keep_nan) ? __builtin_convertvector(f.acc / f.w, f32x4) : f32x4{0.f, 0.f, 0.f, 0.f};
   const int64_t orow = ((int64_t)beta * a.q_len + j) * a.Hq + h, arow = ((int64_t)beta * a.Hq + h) * a.q_len + j;
   if (a.A) *(f32x4*)(a.A + arow * a.d + d0) = out;
   if (a.O) {
@@ -364,7 +368,7 @@ __device__ __forceinline__ void store_merged(const FlatMerge& a, int beta, int h
       *(f32x4*)((float*)a.O + orow * a.d + d0) = out;
     }
   }
-  if (a.LSE && d0 == 0) a.LSE[arow] = f.w > 0 ? f.m + logf((float)f.w) : -INFINITY;
+  if (a.LSE && d0 == 0) a.LSE[arow] = some((float)f.w, a.keep_nan) ? f.m + logf((float)f.w) : -INFINITY;
 }
 
 // A wavefront turns row (beta, h, j) of the call's queries, a lane per pair (bf16, d = 128).  Workgroups

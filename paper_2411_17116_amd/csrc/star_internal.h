@@ -59,6 +59,11 @@ struct SplitPlan {
                        // fp32 kernel: wavefronts that share a 16-row tile (4; anything else: 8)
 };
 
+// A cache held in four bits (q4.h): codes [B, Hkv, cap, d / 2] bytes and exponents [B, Hkv, cap, d / 32] of K and of V.
+struct Q4Rows {
+  void *k_codes, *k_scales, *v_codes, *v_scales;
+};
+
 // Geometry every kernel needs.  Strides are in elements.
 struct Geom {
   int32_t B, Hq, Hkv, G, d;
@@ -194,6 +199,7 @@ struct MergeArgs {
   float* LSE;           // merged), and its log-sum-exp [B, Hq, q_len]; each may be null
   void* Qq;             // with rotary.log2_theta != 0: the call's queries [B, q_len, Hq, 128] in bf16, to be
   Rotary rotary;        // rotated in place (flat plans; the kernels in front have read them as they were)
+  int32_t keep_nan;     // 1: a row with a split whose log-sum-exp is NaN comes out as NaN (0: as zeros)
   int32_t wide;         // 1: the sums of a flat plan in 64 bits
 };
 
@@ -284,6 +290,50 @@ Phase1Plan phase1_plan_f32(const Geom& g);
 hipError_t launch_rope(int dtype, const Geom& g, int H, const void* X, void* Y, const void* K, const void* V,
                        void* Kc, void* Vc, int64_t n_tokens, int64_t dst_row, int64_t pos0, double theta,
                        unsigned int* clear, hipStream_t st);
+// Queries [B, n_tokens, Hq, d] and keys [B, n_tokens, Hkv, d] (null: none) normed per head and rotated: queries into Yq, keys
+// into Yk of the same layout, or (cached) into rows from dst_row of the cache Yk, V as it is into Vc's, or both in four bits into q4.
+struct QkArgs {
+  const void *Q, *K, *V;
+  void *Yq, *Yk, *Vc;
+  Q4Rows q4;
+  int32_t cached;
+  int64_t n_tokens, dst_row;
+  double theta;
+  int64_t pos0;                 // of token 0, where there are no positions
+  const int64_t* positions;     // [B, n_tokens, n_axes], or null
+  int32_t n_axes;
+  uint64_t axis[2];             // of each frequency, two bits
+  const void *q_norm, *k_norm;  // [d], or null
+  float eps;
+  unsigned int* clear;          // as in launch_rope
+};
+hipError_t launch_qk(int dtype, const Geom& g, const QkArgs& q, hipStream_t st);
+
+// n rows of each (batch, head) of K and V, from row `row` of the four-bit cache on, filed or read.  Strides of the plain tensors in
+// elements; row r of the call is row r of theirs.
+struct Q4Copy {
+  Q4Rows q4;
+  void *K, *V;
+  int64_t batch, head, row_stride;
+  int64_t row, n;
+};
+hipError_t launch_q4_store(int dtype, const Geom& g, const Q4Copy& c, hipStream_t st);
+hipError_t launch_q4_load(int dtype, const Geom& g, const Q4Copy& c, hipStream_t st);
+
+// Phase 2 over a cache held in four bits, whose new rows have been filed: O_sub and LSE_sub of `plan`'s splits
+struct Q4Args {
+  Geom g;
+  SplitPlan plan;
+  int64_t cache_len;
+  int32_t q_len, causal;
+  int32_t parts;          // bf16: bf16 parts a weight is taken in, 1 or 2
+  const void* Qq;
+  Q4Rows q4;
+  float* O_sub;
+  float* LSE_sub;
+};
+constexpr int Q4_TILE = 16;            // rows per tile
+hipError_t launch_phase2_q4(int dtype, const Q4Args& a, hipStream_t st);
 hipError_t launch_phase1_f32(const Phase1Args& a, hipStream_t st);
 hipError_t launch_phase2_f32(const Phase2Args& a, hipStream_t st);
 hipError_t launch_phase1_bf16(const Phase1Args& a, hipStream_t st);

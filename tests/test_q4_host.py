@@ -1,0 +1,275 @@
+"""Host side of the four-bit caches and of normed, rotated heads, on the CPU: what is refused, that every argument arrives at its
+place, and that the workspace asked for covers every call."""
+import ctypes
+import random
+
+import pytest
+import torch
+
+import paper_2411_17116_amd as sa
+from paper_2411_17116_amd import binding
+
+INVALID, NULL, DIM, OVERFLOW, SMALL, MISALIGNED = -1, -2, -3, -6, -7, -9
+
+
+def _shape(**kw):
+    return sa.StarShape.make(**{**dict(dtype="bf16", batch=2, n_q_heads=8, n_kv_heads=2, head_dim=128, ctx_len=1024, block=256, anchor=256,
+                                       cache_capacity=1088), **kw})
+
+
+def _rotary(**kw):
+    c = binding.StarRotary(500000.0, 0, None, None, None, 1e-6, 1)
+    for k, v in kw.items():
+        setattr(c, k, v)
+    return c
+
+
+def _axis(i, a):
+    x = (ctypes.c_uint8 * 64)()
+    x[i] = a
+    return x
+
+
+Q4 = binding.StarQ4(0x1000, 0x1000, 0x1000, 0x1000)
+ref = lambda x: None if x is None else ctypes.byref(x)
+
+
+def _qk(shape, rotary, n=4, Q=0x1000, K=0x1000, Yq=0x1000, Yk=0x1000):
+    return sa.load_library().star_attn_qk_norm_rope(ref(shape), ref(rotary), n, Q, K, Yq, Yk, None)
+
+
+def _p1(shape, rotary, Q=0x1000):
+    return sa.load_library().star_attn_phase1_norm_rope(ref(shape), ref(rotary), Q, 0x1000, 0x1000, 0x1000, None, 0x1000, 0x1000, 0x1000, 256, None)
+
+
+def _p2(shape, rotary, L=1024, q=1, Q=0x1000):
+    return sa.load_library().star_attn_phase2_norm_rope(ref(shape), ref(rotary), L, q, Q, 0x1000, 0x1000, 0x1000, 0x1000, None, None, 0x1000, 0x1000,
+                                                        1 << 40, None)
+
+
+def _p4(shape, rotary=None, L=1024, q=1, Q=0x1000, K=0x1000, V=0x1000, c=Q4, Op=None, Lp=None, O=0x1000, ws=0x1000, n=1 << 40):
+    return sa.load_library().star_attn_phase2_q4(ref(shape), ref(rotary), L, q, Q, K, V, ref(c), Op, Lp, O, ws, n, None)
+
+
+def _pair(shape, L=1024, q=1, Q=0x1000, K=None, V=None, c=Q4, A=0x1000, LSE=0x1000, ws=0x1000, n=1 << 40):
+    return sa.load_library().star_attn_phase2_q4_partial(ref(shape), L, q, Q, K, V, ref(c), A, LSE, ws, n, None)
+
+
+def _rows(shape, load, row=0, n=1, K=0x1000, V=0x1000, rows=64, at=0, c=Q4):
+    lib = sa.load_library()
+    if load:
+        return lib.star_attn_q4_load(ref(shape), row, n, ref(c), K, V, rows, at, None)
+    return lib.star_attn_q4_store(ref(shape), row, n, K, V, rows, at, ref(c), None)
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(rope_theta=1.0), INVALID), (dict(rope_theta=float("inf")), INVALID), (dict(pos0=-1), INVALID), (dict(norm_eps=-1e-6), INVALID),
+    (dict(norm_eps=float("nan")), INVALID), (dict(norm_eps=float("inf")), INVALID), (dict(n_axes=0), INVALID), (dict(n_axes=5), INVALID),
+    (dict(axis=_axis(63, 1)), INVALID), (dict(n_axes=2, axis=_axis(0, 2)), INVALID),
+    (dict(positions=0x1008), MISALIGNED), (dict(q_norm=0x1004), MISALIGNED), (dict(k_norm=0x1002), MISALIGNED)])
+def test_a_rotary_out_of_range(kw, code):
+    r = _rotary(**kw)
+    assert _qk(_shape(), r) == _p1(_shape(), r) == _p2(_shape(), r) == _p4(_shape(), r) == code
+
+
+def test_calls_on_projections():
+    r = _rotary()
+    assert _qk(None, r) == _qk(_shape(), None) == _p1(None, None) == _p1(_shape(), None) == _p2(_shape(), None) == NULL
+    assert _qk(_shape(head_dim=64), r) == _p1(_shape(head_dim=64), r) == DIM
+    for n in (0, -1, 1 << 31):
+        assert _qk(_shape(), r, n=n) == INVALID
+    assert _qk(_shape(), r, Q=None, K=None, Yq=None, Yk=None) == NULL
+    assert _qk(_shape(), r, Q=None) == _qk(_shape(), r, Yq=None) == _qk(_shape(), r, K=None) == _qk(_shape(), r, Yk=None) == NULL
+    for arg in ("Q", "K", "Yq", "Yk"):
+        assert _qk(_shape(), r, **{arg: 0x1008}) == MISALIGNED
+    assert _p1(_shape(), r, Q=None) == _p2(_shape(), r, Q=None) == NULL
+    assert _p2(_shape(), r, L=1023) == INVALID and _p2(_shape(), r, q=65) == OVERFLOW
+
+
+@pytest.mark.parametrize("load", [False, True])
+def test_rows(load):
+    s = _shape()
+    assert _rows(None, load) == _rows(s, load, c=None) == _rows(s, load, K=None) == _rows(s, load, V=None) == NULL
+    for field, _ in binding.StarQ4._fields_:
+        for at, code in ((None, NULL), (0x1008, MISALIGNED)):
+            c = binding.StarQ4(0x1000, 0x1000, 0x1000, 0x1000)
+            setattr(c, field, at)
+            assert _rows(s, load, c=c) == _p4(s, c=c) == _pair(s, c=c) == code
+    assert _rows(s, load, K=0x1008) == _rows(s, load, V=0x1001) == MISALIGNED
+    for kw in (dict(n=0), dict(n=-3), dict(row=-1), dict(at=-1), dict(rows=0), dict(rows=1 << 31)):
+        assert _rows(s, load, **kw) == INVALID, kw
+    for kw in (dict(row=1088), dict(row=1088 - 3, n=4), dict(at=64), dict(at=61, n=4), dict(n=65), dict(row=(1 << 63) - 1, n=2, rows=9), dict(n=(1 << 62), rows=1 << 62)):
+        assert _rows(s, load, **kw) == OVERFLOW, kw
+    assert _rows(_shape(batch=60000, n_q_heads=64, n_kv_heads=64, cache_capacity=1 << 20), load, n=1000, rows=1000) == INVALID
+
+
+def test_attention():
+    s = _shape()
+    for arg in ("Q", "K", "V", "O", "ws", "c"):
+        assert _p4(s, **{arg: None}) == NULL, arg
+    assert _p4(s, Op=0x1000) == _p4(s, Lp=0x1000) == _pair(s, K=0x1000) == _pair(s, V=0x1000) == NULL
+    for arg in ("Q", "A", "LSE", "ws", "c"):
+        assert _pair(s, **{arg: None}) == NULL, arg
+    for arg in ("Q", "K", "V", "O", "ws"):
+        assert _p4(s, **{arg: 0x1008}) == MISALIGNED, arg
+    assert _p4(s, ws=0x1010) == _p4(s, Op=0x1008, Lp=0x1000) == _p4(s, Op=0x1000, Lp=0x1002) == _pair(s, A=0x1008) == _pair(s, LSE=0x1001) == MISALIGNED
+    assert _p4(s, q=0) == _p4(s, q=(1 << 20) + 1) == _p4(s, L=1023) == _pair(s, L=1000) == INVALID
+    assert _p4(s, q=65) == _p4(s, L=1088) == _pair(s, L=1089) == OVERFLOW
+    assert _p4(s, n=255) == _pair(s, n=0) == SMALL
+    need = sa.phase2_q4_plan(s, 1024, 7).workspace_bytes
+    assert _p4(s, q=7, n=need - 1) == SMALL
+    assert _p4(_shape(dtype=3)) == -4 and _p4(_shape(head_dim=64)) == DIM
+
+
+def test_the_workspace_asked_for_covers_every_call():
+    rng = random.Random(7)
+    for _ in range(150):
+        fp32, hkv = rng.random() < 0.4, rng.choice([1, 2, 3, 8, 16, 40])
+        L = int(2 ** rng.uniform(0, 19))
+        tail = int(2 ** rng.uniform(3, 13))
+        s = sa.StarShape.make("fp32" if fp32 else "bf16", rng.choice([1, 1, 2, 7, 64]), hkv * rng.choice([1, 2, 3, 4, 8, 16]), hkv,
+                              rng.choice([64, 128]) if fp32 else 128, L, max(1, int(L / 2 ** rng.uniform(-1, 6))), 0, L + tail)
+        top = rng.choice([1, 2, 7, 33, 100, 256, tail])
+        have = sa.q4_workspace_bytes(s, min(top, tail))
+        for _ in range(25):
+            q = rng.randint(1, min(top, tail))
+            at = rng.randint(L, L + tail - q)
+            for parts in (False, True):
+                p = sa.phase2_q4_plan(s, at, q, parts)
+                assert p.workspace_bytes <= have, (s.batch, s.n_q_heads, hkv, s.head_dim, L, s.block, tail, top, q, at, parts)
+                assert p.n_splits >= 1 and (p.flat == 1) == (not parts) and (parts or (p.n_splits - 1) * p.split_len < at + q <= p.n_splits * p.split_len)
+    assert sa.q4_workspace_bytes(_shape(head_dim=64), 4) == sa.q4_workspace_bytes(_shape(), 0) == 0
+
+
+# ------------------------------------------------------------------ the binding
+
+
+class Stream:
+    cuda_stream = 0x7700
+
+
+NAMES = ("qk_norm_rope", "phase1_norm_rope", "phase2_norm_rope", "q4_store", "q4_load", "phase2_q4", "phase2_q4_partial")
+OTHERS = ("phase1", "phase1_anchor", "phase1_rope", "phase2", "phase2_rope", "phase2_static", "phase2_partial", "merge", "rope")
+
+
+@pytest.fixture(params=["extension", "ctypes"])
+def seen(request, monkeypatch):
+    """Entry points that note what they are called with."""
+    lib, log, keep = sa.load_library(), {}, []
+
+    class Fake:
+        pass
+
+    fake = Fake()
+    for name in OTHERS:
+        setattr(fake, "star_attn_" + name, getattr(lib, "star_attn_" + name))
+    for name in NAMES:
+        real = getattr(lib, "star_attn_" + name)
+
+        def call(*args, name=name):
+            log[name] = (ctypes.cast(args[0], ctypes.POINTER(sa.StarShape)).contents.ctx_len,) + args[1:]
+            return 0
+
+        fn = ctypes.CFUNCTYPE(ctypes.c_int, *[ctypes.c_void_p if hasattr(k, "contents") else k for k in real.argtypes])(call)
+        keep.append(fn)
+        setattr(fake, "star_attn_" + name, fn)
+    if request.param == "ctypes":
+        monkeypatch.setattr(binding, "_MARSHAL", binding._CtypesCalls(fake))
+        yield log
+        return
+    binding._calls()
+    binding._bind(fake)
+    yield log
+    binding._bind(lib)
+
+
+def _at(address, Struct):
+    return ctypes.cast(address, ctypes.POINTER(Struct)).contents
+
+
+def test_every_argument_at_its_place(seen):
+    s = _shape(batch=2, ctx_len=1000)
+    t = lambda *dims: torch.zeros(dims or (2, 3, 8, 128), dtype=torch.bfloat16)
+    Q, K, V, O, L, Kc, Vc, Op, Lp, A = (t() for _ in range(10))
+    ws, st = torch.zeros(24, dtype=torch.int16), Stream()
+    p = lambda *ts: tuple(x.data_ptr() for x in ts)
+    w, v, at = t(128), t(128), torch.zeros((2, 3, 3), dtype=torch.int64)
+    r = sa.Rotary(5e5, q_norm=w, k_norm=v, eps=0.5, pos0=9, positions=at, sections=[16, 24, 24])
+    assert (r.c.rope_theta, r.c.pos0, r.c.norm_eps, r.c.n_axes) == (5e5, 9, 0.5, 3)
+    assert (r.c.positions, r.c.q_norm, r.c.k_norm) == p(at, w, v)
+    assert list(r.c.axis) == [0] * 16 + [1] * 24 + [2] * 24
+    cache = sa.alloc_q4_cache(s, device="cpu")
+    assert [cache.c.k_codes, cache.c.k_scales, cache.c.v_codes, cache.c.v_scales] == list(p(cache.k_codes, cache.k_scales, cache.v_codes, cache.v_scales))
+
+    def struct(x, Struct, want):
+        got = _at(x, Struct)
+        return all(list(getattr(got, n)) == list(getattr(want, n)) if n == "axis" else getattr(got, n) == getattr(want, n) for n, _ in Struct._fields_)
+
+    sa.qk_norm_rope(s, r, Q, K, O, L, stream=st)
+    a = seen["qk_norm_rope"]
+    assert a[:1] + a[2:] == (1000, 3, *p(Q, K, O, L), 0x7700) and struct(a[1], binding.StarRotary, r.c)
+    sa.qk_norm_rope(s, r, None, K, None, L, stream=st)
+    assert seen["qk_norm_rope"][2:] == (3, None, K.data_ptr(), None, L.data_ptr(), 0x7700)
+    long = sa.Rotary(5e5)
+    sa.phase1_norm_rope(s, long, Q, K, V, O, Kc, Vc, LSE_ctx=L, workspace=ws, stream=st)
+    a = seen["phase1_norm_rope"]
+    assert a[:1] + a[2:] == (1000, *p(Q, K, V, O, L, Kc, Vc, ws), 48, 0x7700) and struct(a[1], binding.StarRotary, long.c)
+    sa.phase2_norm_rope(s, r, 1010, Q, K, V, Kc, Vc, O, ws, O_part=Op, LSE_part=Lp, stream=st)
+    a = seen["phase2_norm_rope"]
+    assert a[:1] + a[2:] == (1000, 1010, 3, *p(Q, K, V, Kc, Vc, Op, Lp, O, ws), 48, 0x7700) and struct(a[1], binding.StarRotary, r.c)
+    rows = t(2, 2, 77, 128)
+    sa.q4_store(s, 5, 6, rows, V, cache, plain_row=7, stream=st)
+    a = seen["q4_store"]
+    assert a[:7] + a[8:] == (1000, 5, 6, *p(rows, V), 77, 7, 0x7700) and struct(a[7], binding.StarQ4, cache.c)
+    sa.q4_load(s, 5, 6, cache, rows, V, stream=st)
+    a = seen["q4_load"]
+    assert a[:3] + a[4:] == (1000, 5, 6, *p(rows, V), 77, 5, 0x7700) and struct(a[3], binding.StarQ4, cache.c)
+    sa.phase2_q4(s, 1010, Q, K, V, cache, O, ws, O_part=Op, LSE_part=Lp, stream=st)
+    a = seen["phase2_q4"]
+    assert a[:7] + a[8:] == (1000, None, 1010, 3, *p(Q, K, V), *p(Op, Lp, O, ws), 48, 0x7700) and struct(a[7], binding.StarQ4, cache.c)
+    sa.phase2_q4(s, 1010, Q, K, V, cache, O, ws, rotary=r, stream=st)
+    a = seen["phase2_q4"]
+    assert struct(a[1], binding.StarRotary, r.c) and a[8:11] == (None, None, O.data_ptr())
+    sa.phase2_q4_partial(s, 1010, Q, cache, A, L, ws, Kq=K, Vq=V, stream=st)
+    a = seen["phase2_q4_partial"]
+    assert a[:6] + a[7:] == (1000, 1010, 3, *p(Q, K, V), *p(A, L, ws), 48, 0x7700) and struct(a[6], binding.StarQ4, cache.c)
+    sa.phase2_q4_partial(s, 1010, Q, cache, A, L, ws, stream=st)
+    assert seen["phase2_q4_partial"][4:6] == (None, None)
+
+
+def test_what_the_binding_refuses(seen):
+    s, st = _shape(), Stream()
+    t = lambda *dims: torch.zeros(dims or (2, 3, 8, 128), dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="contiguous"):
+        sa.qk_norm_rope(s, sa.Rotary(5e5), t().transpose(1, 2), t(), t(), t(), stream=st)
+    with pytest.raises(ValueError, match="contiguous"):
+        sa.Rotary(5e5, positions=torch.zeros((3, 2, 2), dtype=torch.int64).transpose(0, 1))
+    with pytest.raises(ValueError):
+        sa.Rotary(5e5, positions=torch.zeros((2, 3, 2), dtype=torch.int32))
+    with pytest.raises(ValueError):
+        sa.Rotary(5e5, positions=torch.zeros((2, 3, 2), dtype=torch.int64), sections=[16, 24, 24])
+    with pytest.raises(ValueError):
+        sa.Rotary(5e5, sections=[16, 24, 23])
+    with pytest.raises(ValueError):
+        sa.Rotary(5e5, sections=[32, 32], axis=[0] * 64)
+    with pytest.raises(ValueError):
+        sa.Rotary(5e5, q_norm=t(1, 128))
+    for r in (sa.Rotary(5e5, q_norm=t(64)), sa.Rotary(5e5, k_norm=t(128).float()), sa.Rotary(5e5, sections=[16, 16]),
+              sa.Rotary(5e5, positions=torch.zeros((2, 4), dtype=torch.int64)), sa.Rotary(5e5, positions=torch.zeros((1, 3, 1), dtype=torch.int64))):
+        with pytest.raises(ValueError):
+            sa.qk_norm_rope(s, r, t(), t(), t(), t(), stream=st)
+    cache = sa.alloc_q4_cache(s, device="cpu")
+    with pytest.raises(ValueError):
+        sa.Q4Cache(s, cache.k_scales, cache.k_codes, cache.v_codes, cache.v_scales)
+    with pytest.raises(ValueError):
+        sa.Q4Cache(s, cache.k_codes.to(torch.int8), cache.k_scales, cache.v_codes, cache.v_scales)
+    with pytest.raises(ValueError):
+        sa.phase2_q4(_shape(cache_capacity=1089), 1024, t(), t(), t(), cache, t(), t(), stream=st)
+    with pytest.raises((AttributeError, TypeError)):
+        sa.phase2_q4(s, 1024, t(), t(), t(), None, t(), t(), stream=st)
+    assert not seen
+
+
+def test_structs_as_the_header_has_them():
+    assert ctypes.sizeof(binding.StarRotary) == 112 and binding.StarRotary.norm_eps.offset == 40 and binding.StarRotary.axis.offset == 48
+    assert ctypes.sizeof(binding.StarQ4) == 32
