@@ -447,17 +447,18 @@ static bool make_plan(const star_attn_shape* s, int64_t q_len, int64_t total, bo
   return true;
 }
 
-// ---- four-bit cache: workgroups of 16 rows and a split, two of them on a CU.
+// ---- four-bit cache: workgroups of 16 or 32 rows and a split
 constexpr int64_t Q4_WGS = 512;
 constexpr int64_t Q4_SPLIT_MIN = 128;      // keys: a unit of 32 for each of four wavefronts
+static int q4_tile(const Geom& g, int64_t q_len) { return (int64_t)g.G * q_len <= 16 ? 16 : 32; }
 static int64_t q4_splits(const Geom& g, int64_t q_len) {
-  const int64_t wgs = (int64_t)g.B * g.Hkv * ceil_div((int64_t)g.G * q_len, Q4_TILE);
+  const int64_t wgs = (int64_t)g.B * g.Hkv * ceil_div((int64_t)g.G * q_len, q4_tile(g, q_len));
   return wgs < Q4_WGS ? Q4_WGS / wgs : 1;
 }
 static bool make_q4_plan(const Geom& g, int64_t q_len, int64_t total, bool want_parts, SplitPlan* p) {
   *p = SplitPlan{};
   const int64_t n = ceil_div(g.L, g.b), want = q4_splits(g, q_len);
-  p->tile_rows = Q4_TILE;
+  p->tile_rows = q4_tile(g, q_len);
   p->n_blocks = (int32_t)n;
   if (n > (1 << 24)) return false;
   if (!want_parts) {
@@ -1019,23 +1020,19 @@ static int phase2_q4_impl(const star_attn_shape* shape, const star_attn_rotary* 
   hipStream_t st = (hipStream_t)hip_stream;
   const Q4Rows q4 = {cache->k_codes, cache->k_scales, cache->v_codes, cache->v_scales};
 
-  // Algorithm 2: the new tokens join the cache before they attend
-  if (append) {
-    hipError_t e;
-    if (rotary) {
-      QkArgs q = qk_args(*rotary, q_len, rotary->pos0 + cache_len);
-      q.Q = Qq; q.Yq = Qq; q.K = Kq; q.V = Vq; q.q4 = q4; q.dst_row = cache_len;
-      e = launch_qk(shape->dtype, g, q, st);
-    } else {
-      const Q4Copy c = {q4, const_cast<void*>(Kq), const_cast<void*>(Vq), q_len * g.Hkv * g.d, g.d, (int64_t)g.Hkv * g.d, cache_len, q_len};
-      e = launch_q4_store(shape->dtype, g, c, st);
-    }
-    if (e != hipSuccess) return STAR_ATTN_ERR_LAUNCH_FAILED;
+  // Algorithm 2: the new tokens join the cache before they attend; the attention kernel files them itself, unless they are
+  // rotated first
+  if (append && rotary) {
+    QkArgs q = qk_args(*rotary, q_len, rotary->pos0 + cache_len);
+    q.Q = Qq; q.Yq = Qq; q.K = Kq; q.V = Vq; q.q4 = q4; q.dst_row = cache_len;
+    if (launch_qk(shape->dtype, g, q, st) != hipSuccess) return STAR_ATTN_ERR_LAUNCH_FAILED;
   }
   Q4Args a;
   a.g = g; a.plan = plan; a.cache_len = cache_len; a.q_len = (int32_t)q_len; a.causal = append ? 1 : 0;
   a.parts = pair || O_part ? 2 : 1;        // (weights in bf16 are what bf16 outputs show; fp32 ones are held to more)
   a.Qq = Qq; a.q4 = q4;
+  a.Kn = append && !rotary ? Kq : nullptr;
+  a.Vn = append && !rotary ? Vq : nullptr;
   a.O_sub = (float*)workspace;
   a.LSE_sub = (float*)workspace + rows * plan.s_total * g.d;
   if (launch_phase2_q4(shape->dtype, a, st) != hipSuccess) return STAR_ATTN_ERR_LAUNCH_FAILED;
@@ -1079,8 +1076,10 @@ size_t star_attn_q4_workspace_bytes(const star_attn_shape* shape, int64_t max_q_
   };
   const int64_t pairs = (int64_t)g.B * g.Hkv;
   for (int64_t want = 1; want * pairs <= Q4_WGS; ++want) {
-    const int64_t q = Q4_WGS / (pairs * want) * Q4_TILE / g.G;
-    if (q >= 1) consider(q < max_q_len ? q : max_q_len);
+    for (int tile = 16; tile <= 32; tile += 16) {
+      const int64_t q = (tile == 16 ? 1 : Q4_WGS / (pairs * want)) * tile / g.G;
+      if (q >= 1) consider(q < max_q_len ? q : max_q_len);
+    }
   }
   consider(max_q_len);
   return best;

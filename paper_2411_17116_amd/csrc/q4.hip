@@ -111,10 +111,20 @@ hipError_t launch_rows(int dtype, const Geom& g, const Q4Copy& c, hipStream_t st
   return g.d == 64 ? launch_rows<float, 64, LOAD>(a, st) : launch_rows<float, 128, LOAD>(a, st);
 }
 
-// ------------------------------------------------------------------ attention
-// chunk c (16 bytes) of key row r of V sits in slot c ^ swz(r): what rows of 16 chunks (8) are spread by
-template <int D>
-__device__ __forceinline__ int swz(int r) { return D == 128 ? ((r << 1) & 15) | ((r >> 3) & 1) : r & 7; }
+// ------------------------------------------------------------------ attention, few rows
+// A call of up to 32 rows (token x head of a KV group) reads every code once and does 16 to 128 flops per byte: a stream, bound by HBM.
+//   * A workgroup is four wavefronts that share a split and meet in LDS behind the key loop; without per-part outputs the wavefronts of a
+//     KV head take the comb of 32-key units w, w + N, w + 2N, .., so that together they read one contiguous window of its cache.
+//   * A lane has D / 4 elements of a key (with 128 of them a group: 16 bytes of codes and a byte of exponent), straight from the cache in the layout that the MFMA wants of
+//     K; two units are in registers, and a unit's are requested again as soon as its K is multiplied and its V in LDS.
+//   * S^T = K Q^T in bf16 products, which lose nothing: a four-bit value is a bf16 number, an fp32 query three of them.  (The instruction that
+//     multiplies four-bit codes as they are, by queries in two 8-bit parts, adds up a group's products in fewer bits: 2^-11 of sum |q k| off with
+//     queries of different sizes.)  The exponentiated unit is the B operand of O^T += V^T P^T, weights in PP bf16 parts, V by way of LDS to be read back transposed.
+//   * The call's own keys are put into four bits by the wavefront whose unit has them, which files them and attends to them from its registers.
+
+// chunk c (16 bytes) of V's row r sits in slot c ^ (r & 7): eight rows' chunk, which eight lanes write at once, lie in eight different ones, as do
+// the two chunks of four rows that a transposing read of sixteen lanes takes with its neighbours'
+__device__ __forceinline__ int swz(int r) { return r & 7; }
 
 __device__ __forceinline__ float xor16(float x) { return __int_as_float(__builtin_amdgcn_ds_swizzle(__float_as_int(x), 0x401F)); }
 __device__ __forceinline__ float xor32_max(float x) {
@@ -126,6 +136,11 @@ __device__ __forceinline__ float xor32_sum(float x) {
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
+constexpr int WAVES = 4;
+constexpr int UNIT = 32;              // keys a wavefront takes at once
+
+typedef const __attribute__((address_space(1))) unsigned char* GlobalBytes;
+
 // What a lane holds of 16 keys of K or of V: D / 4 elements of key lane % 16, from D / 4 * (lane / 16) on, and their unit.
 template <int D>
 struct Rows16 {
@@ -133,13 +148,28 @@ struct Rows16 {
   uint32_t e;
 };
 template <int D>
-__device__ __forceinline__ Rows16<D> load_rows(const unsigned char* codes, const unsigned char* scales, size_t row, int j4) {
-  Rows16<D> x;
-  const unsigned char* p = codes + row * (D / 2) + j4 * (D / 8);
+struct UnitRegs {
+  Rows16<D> k[2], v[2];
+};
+template <typename V, bool NT>
+__device__ __forceinline__ V fetch(GlobalBytes p) {
+  const __attribute__((address_space(1))) V* q = (const __attribute__((address_space(1))) V*)p;
+  return NT ? __builtin_nontemporal_load(q) : *q;
+}
+typedef __attribute__((ext_vector_type(2))) int i32x2;
+// (codes and exponents of the lane's key; codes' rows are D / 2 bytes, exponents' D / 32)
+template <int D, bool NT>
+__device__ __forceinline__ void load_rows(Rows16<D>& x, GlobalBytes codes, GlobalBytes scales) {
+  if constexpr (D == 128) {
+    const i32x4 c = fetch<i32x4, NT>(codes);
 #pragma unroll
-  for (int i = 0; i < D / 32; ++i) x.c[i] = ((const uint32_t*)p)[i];
-  x.e = scales[row * (D / 32) + (D == 128 ? j4 : j4 >> 1)];
-  return x;
+    for (int i = 0; i < 4; ++i) x.c[i] = (uint32_t)c[i];
+  } else {
+    const i32x2 c = fetch<i32x2, NT>(codes);
+    x.c[0] = (uint32_t)c[0];
+    x.c[1] = (uint32_t)c[1];
+  }
+  x.e = fetch<unsigned char, NT>(scales);
 }
 __device__ __forceinline__ bf16x8 values(uint32_t c, float unit) {
   const q4_bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, unit, 0), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, unit, 1);
@@ -166,24 +196,24 @@ __device__ __forceinline__ void split(float x, __bf16 (&p)[P]) {
   }
 }
 
-constexpr int WAVES = 4;
-constexpr int UNIT = 32;              // keys a wavefront takes at once
-
-struct TileDiv {
-  Div Hkv, tiles, splits, G;
+template <int QP, int NT, int DT, int RB>
+struct StreamState {
+  bf16x8 q[RB][QP][NT];   // Q^T fragments: D / 4 (lane / 16) + 8 t ..+7 of row lane % 16
+  f32x4 o[RB][DT];        // O^T: element 16 dt + 4 (lane / 16) + v of that row
+  float m[RB], l[RB], neg[RB];      // running maximum of the logits, this lane's share of the sum, -m c (0 while nothing was visible)
 };
 
-// A workgroup of four wavefronts has 16 rows (token x head of a KV group) and a split of the cache, whose units of 32 keys they take
-// in turn; their results meet in LDS.  S^T = K Q^T in bf16 products, which are exact: a four-bit value is a bf16 number, fp32 queries are
-// three of them.  The exponentiated tile is the B operand of O^T += V^T P^T, weights in PP bf16 parts; V goes through LDS to
-// be read back transposed.
-template <typename T, int D, int PP>
-__global__ __launch_bounds__(64 * WAVES) void q4_attend_kernel(Q4Args a, TileDiv by, unsigned first_wg) {
-  constexpr int QP = sizeof(T) == 2 ? 1 : 3, NT = D / 32, DT = D / 16, ROWB = 2 * D;
-  __shared__ __attribute__((aligned(1024))) char lds_v[WAVES][UNIT * ROWB];
-  __shared__ float lds_m[WAVES][16], lds_l[WAVES][16];
+struct StreamDiv {
+  Div Hkv, tiles, splits, G, steps;      // steps between two of a wavefront's (flat plans): splits times wavefronts
+};
+
+template <typename T, int D, int PP, int RB, bool NT>
+__global__ __launch_bounds__(64 * WAVES, RB == 1 && sizeof(T) == 2 ? 3 : 2) void q4_stream_kernel(Q4Args a, StreamDiv by, unsigned first_wg) {
+  constexpr int QP = sizeof(T) == 2 ? 1 : 3, NS = D / 32, DT = D / 16, ROWB = 2 * D;
+  __shared__ __attribute__((aligned(1024))) char lds_v[WAVES][UNIT * ROWB];      // 16 rows of D floats of a wavefront, too
+  __shared__ float lds_m[WAVES][16 * RB], lds_l[WAVES][16 * RB];
   const Geom& g = a.g;
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, qc = lane & 15, j4 = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, qc = lane & 15, j4 = lane >> 4;
   uint32_t w = first_wg + blockIdx.x;
   uint32_t x = quotient(w, by.Hkv);
   const uint32_t kvh = w - x * by.Hkv.d;
@@ -192,63 +222,228 @@ __global__ __launch_bounds__(64 * WAVES) void q4_attend_kernel(Q4Args a, TileDiv
   x = quotient(w, by.splits);
   const uint32_t sp = w - x * by.splits.d, beta = x;
 
-  const int row = tile * 16 + qc, R = g.G * a.q_len;
-  const bool live = row < R;
-  const int j = live ? (int)quotient(row, by.G) : 0, head = kvh * g.G + (live ? row - j * g.G : 0);
-  const int total = (int)(a.cache_len + (a.causal ? a.q_len : 0));
-  int64_t lo64, hi64;
-  split_range(a.plan, g.L, g.b, total, sp, &lo64, &hi64);
-  const int lo = (int)lo64, hi = (int)hi64;
-  const int lim0 = a.causal ? (int)a.cache_len + j + 1 : (int)a.cache_len, lim = lim0 < hi ? lim0 : hi;
-
-  bf16x8 q[QP][NT];
-  {
-    const T* p = (const T*)a.Qq + (((size_t)beta * a.q_len + j) * g.Hq + head) * D + j4 * (D / 4);
+  const int R = g.G * a.q_len;
+  int j[RB], head[RB];
+  bool live[RB];
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
+  for (int b = 0; b < RB; ++b) {
+    const int row = tile * 16 * RB + 16 * b + qc;
+    live[b] = row < R;
+    j[b] = live[b] ? (int)quotient(row, by.G) : 0;
+    head[b] = kvh * g.G + (live[b] ? row - j[b] * g.G : 0);
+  }
+  const int cache_len = (int)a.cache_len, total = cache_len + (a.causal ? a.q_len : 0);
+  const int cached = a.Kn ? cache_len : total;
+  // unit `s` of this wavefront is keys [base + s stride, + 32) below hi; the first n_whole are cached and seen by every row as a whole
+  const int free_hi = a.causal && cache_len + 1 < cached ? cache_len + 1 : cached;
+  int base, stride, n_units, n_whole, hi;
+  if (a.plan.flat) {
+    const int all = a.plan.s_total * WAVES, first = sp * WAVES + wave, T_ = (total + UNIT - 1) / UNIT, whole = free_hi / UNIT;
+    base = first * UNIT;
+    stride = all * UNIT;
+    n_units = first < T_ ? (int)quotient(T_ - first + all - 1, by.steps) : 0;
+    n_whole = first < whole ? (int)quotient(whole - first + all - 1, by.steps) : 0;
+    hi = total;
+  } else {
+    int64_t lo64, hi64;
+    split_range(a.plan, g.L, g.b, total, sp, &lo64, &hi64);
+    hi = (int)hi64;
+    base = (int)lo64 + UNIT * wave;
+    stride = UNIT * WAVES;
+    n_units = hi > base ? (hi - base + stride - 1) / stride : 0;
+    const int room = (free_hi < hi ? free_hi : hi) - UNIT - base;
+    n_whole = room >= 0 ? room / stride + 1 : 0;
+  }
+
+  const size_t pair = (size_t)beta * g.Hkv + kvh, rows0 = pair * (size_t)g.cap;
+  GlobalBytes kc = (GlobalBytes)a.q4.k_codes + rows0 * (D / 2), ks = (GlobalBytes)a.q4.k_scales + rows0 * (D / 32);
+  GlobalBytes vc = (GlobalBytes)a.q4.v_codes + rows0 * (D / 2), vs = (GlobalBytes)a.q4.v_scales + rows0 * (D / 32);
+  const int group = D == 128 ? j4 : j4 >> 1;
+  const unsigned c_off = qc * (D / 2) + j4 * (D / 8), s_off = qc * (D / 32) + group;
+  const auto load_whole = [&](UnitRegs<D>& u, int s) {
+    const int key0 = base + s * stride;
+    GlobalBytes a0 = kc + (size_t)key0 * (D / 2), a1 = ks + (size_t)key0 * (D / 32), a2 = vc + (size_t)key0 * (D / 2), a3 = vs + (size_t)key0 * (D / 32);
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt) load_rows<D, NT>(u.k[kt], a0 + kt * 16 * (D / 2) + c_off, a1 + kt * 16 * (D / 32) + s_off);
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt) load_rows<D, NT>(u.v[kt], a2 + kt * 16 * (D / 2) + c_off, a3 + kt * 16 * (D / 32) + s_off);
+  };
+
+  UnitRegs<D> u0, u1;
+  if (0 < n_whole) load_whole(u0, 0);
+  if (1 < n_whole) load_whole(u1, 1);
+  StreamState<QP, NS, DT, RB> st;
+#pragma unroll
+  for (int b = 0; b < RB; ++b) {
+    const T* p = (const T*)a.Qq + (((size_t)beta * a.q_len + j[b]) * g.Hq + head[b]) * D + j4 * (D / 4);
+#pragma unroll
+    for (int t = 0; t < NS; ++t) {
       float y[8];
       load8(p + 8 * t, y);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         __bf16 part[QP];
-        split<QP>(live ? y[e] : 0.f, part);
+        split<QP>(live[b] ? y[e] : 0.f, part);
 #pragma unroll
-        for (int i = 0; i < QP; ++i) q[i][t][e] = part[i];
+        for (int i = 0; i < QP; ++i) st.q[b][i][t][e] = part[i];
       }
     }
-  }
-  f32x4 o[DT];
 #pragma unroll
-  for (int dt = 0; dt < DT; ++dt) o[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
-  float m = -INFINITY, l = 0.f;
+    for (int dt = 0; dt < DT; ++dt) st.o[b][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    st.m[b] = -INFINITY;
+    st.l[b] = st.neg[b] = 0.f;
+  }
   const float c = g.scale * LOG2E;
-
-  const size_t base = ((size_t)beta * g.Hkv + kvh) * (size_t)g.cap;
-  const unsigned char *kc = (const unsigned char*)a.q4.k_codes, *ks = (const unsigned char*)a.q4.k_scales;
-  const unsigned char *vc = (const unsigned char*)a.q4.v_codes, *vs = (const unsigned char*)a.q4.v_scales;
   char* vl = lds_v[wave];
   const unsigned lds0 = (unsigned)(size_t)(LDS_AS char*)vl;
+  unsigned vw[NS];                      // (row qc of the first 16; the others' are 16 rows further, 16 being 0 modulo 8)
+#pragma unroll
+  for (int t = 0; t < NS; ++t) vw[t] = lds0 + qc * ROWB + (((j4 * NS + t) ^ swz(qc)) << 4);
+  const int rr = 4 * j4 + (qc >> 2);
+  unsigned vr[DT];
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt) vr[dt] = lds0 + rr * ROWB + (((2 * dt + ((lane & 3) >> 1)) ^ swz(rr)) << 4) + 8 * (lane & 1);
 
-  for (int key0 = lo + UNIT * wave; key0 < hi; key0 += UNIT * WAVES) {
-    // keys past the last are that one again, masked below
-    Rows16<D> k[2], v[2];
-    f32x4 s[2];
+  // A unit's scores, and V into LDS: its registers are then free.
+  f32x4 s[RB][2];
+  const auto score = [&](const UnitRegs<D>& u) {
 #pragma unroll
     for (int kt = 0; kt < 2; ++kt) {
-      const int key = key0 + 16 * kt + qc;
-      const size_t r = base + (key < hi ? key : hi - 1);
-      k[kt] = load_rows<D>(kc, ks, r, j4);
-      v[kt] = load_rows<D>(vc, vs, r, j4);
+      const float unit = q4_unit_value(u.k[kt].e);
+#pragma unroll
+      for (int t = 0; t < NS; ++t) {
+        const bf16x8 y = values(u.k[kt].c[t], unit);
+#pragma unroll
+        for (int b = 0; b < RB; ++b)
+#pragma unroll
+          for (int i = QP - 1; i >= 0; --i) {
+            const f32x4 acc = t == 0 && i == QP - 1 ? f32x4{0.f, 0.f, 0.f, 0.f} : s[b][kt];
+            s[b][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(y, st.q[b][i][t], acc, 0, 0, 0);
+          }
+      }
     }
 #pragma unroll
     for (int kt = 0; kt < 2; ++kt) {
-      const float unit = q4_unit_value(k[kt].e);
-      s[kt] = f32x4{0.f, 0.f, 0.f, 0.f};
+      const float unit = q4_unit_value(u.v[kt].e);
 #pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        const bf16x8 y = values(k[kt].c[t], unit);
+      for (int t = 0; t < NS; ++t) *(LDS_AS bf16x8*)(size_t)(vw[t] + kt * 16 * ROWB) = values(u.v[kt].c[t], unit);
+    }
+  };
+  // Then softmax and products.
+  const auto attend = [&] {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    bf16x8 v[DT];
 #pragma unroll
-        for (int i = QP - 1; i >= 0; --i) s[kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(y, q[i][t], s[kt], 0, 0, 0);
+    for (int dt = 0; dt < DT; ++dt) {
+      const s16x4 y0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4*)(size_t)vr[dt]);
+      const s16x4 y1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4*)(size_t)(vr[dt] + 16 * ROWB));
+      v[dt] = __builtin_shufflevector(__builtin_bit_cast(bf16x4, y0), __builtin_bit_cast(bf16x4, y1), 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+    bf16x8 p[RB][PP];
+#pragma unroll
+    for (int b = 0; b < RB; ++b) {
+      const float tmax = fmaxf(fmaxf(fmaxf(s[b][0][0], s[b][0][1]), fmaxf(s[b][0][2], s[b][0][3])),
+                               fmaxf(fmaxf(s[b][1][0], s[b][1][1]), fmaxf(s[b][1][2], s[b][1][3])));
+      // lanes exchange their maxima only where some row's moves
+      if (__builtin_amdgcn_ballot_w64(tmax > st.m[b]) != 0) {
+        const float m = fmaxf(st.m[b], xor32_max(fmaxf(tmax, xor16(tmax)))), mm = m == -INFINITY ? 0.f : m;
+        const float alpha = __builtin_amdgcn_exp2f((st.m[b] - mm) * c);
+        st.l[b] *= alpha;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) st.o[b][dt] *= alpha;
+        st.m[b] = m;
+        st.neg[b] = mm * -c;
+      }
+      float sum = 0.f;
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][kt][e], c, st.neg[b]));
+          sum += y;
+          __bf16 part[PP];
+          split<PP>(y, part);
+#pragma unroll
+          for (int i = 0; i < PP; ++i) p[b][i][4 * kt + e] = part[i];
+        }
+      st.l[b] += sum;
+    }
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int b = 0; b < RB; ++b)
+#pragma unroll
+        for (int i = PP - 1; i >= 0; --i) st.o[b][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[dt], p[b][i], st.o[b][dt], 0, 0, 0);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  };
+  int n = 0;
+  for (; n + 1 < n_whole; n += 2) {
+    score(u0);
+    if (n + 2 < n_whole) load_whole(u0, n + 2);
+    attend();
+    score(u1);
+    if (n + 3 < n_whole) load_whole(u1, n + 3);
+    attend();
+  }
+  if (n < n_whole) {
+    score(u0);
+    attend();
+  }
+  // The units that end past `hi` or among the call's tokens, or that not every row sees.
+  int lim[RB];
+#pragma unroll
+  for (int b = 0; b < RB; ++b) {
+    const int end = a.causal ? cache_len + j[b] + 1 : total;
+    lim[b] = !live[b] ? 0 : end < hi ? end : hi;
+  }
+  for (n = n_whole; n < n_units; ++n) {
+    const int key0 = base + n * stride;
+    UnitRegs<D> u;
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt) {
+      int key = key0 + 16 * kt + qc;
+      const bool there = key < hi;                 // keys past the last are that one again, masked below
+      key = there ? key : hi - 1;
+      if (key < cached) {
+        load_rows<D, false>(u.k[kt], kc + (size_t)key * (D / 2) + j4 * (D / 8), ks + (size_t)key * (D / 32) + group);
+        load_rows<D, false>(u.v[kt], vc + (size_t)key * (D / 2) + j4 * (D / 8), vs + (size_t)key * (D / 32) + group);
+      }
+      if (__builtin_amdgcn_ballot_w64(key >= cached) != 0) {
+        // (all lanes, so that the lanes of a group meet; those of cached keys keep what they have)
+        const size_t from = (((size_t)beta * a.q_len + (key < cached ? 0 : key - cached)) * g.Hkv + kvh) * D + j4 * (D / 4);
+        const T* src[2] = {(const T*)a.Kn + from, (const T*)a.Vn + from};
+        Rows16<D>* to[2] = {&u.k[kt], &u.v[kt]};
+        unsigned char* codes[2] = {(unsigned char*)a.q4.k_codes, (unsigned char*)a.q4.v_codes};
+        unsigned char* scales[2] = {(unsigned char*)a.q4.k_scales, (unsigned char*)a.q4.v_scales};
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          float y[NS][8];
+          uint32_t most = 0;
+#pragma unroll
+          for (int t = 0; t < NS; ++t) {
+            load8(src[i] + 8 * t, y[t]);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) most = magnitude_bits(y[t][e]) > most ? magnitude_bits(y[t][e]) : most;
+          }
+          if (D == 64) {
+            const uint32_t other = (uint32_t)__shfl_xor((int)most, 16);
+            most = other > most ? other : most;
+          }
+          Rows16<D> r;
+          r.e = q4_unit(most);
+#pragma unroll
+          for (int t = 0; t < NS; ++t) r.c[t] = r.e == 255u ? 0u : q4_codes(y[t], q4_unit_value(r.e));
+          if (key < cached) continue;
+          *to[i] = r;
+          if (there && tile == 0) {
+            unsigned char* at = codes[i] + (rows0 + key) * (D / 2) + j4 * (D / 8);
+            if constexpr (D == 128) *(i32x4*)at = i32x4{(int)r.c[0], (int)r.c[1], (int)r.c[2], (int)r.c[3]};
+            else *(i32x2*)at = i32x2{(int)r.c[0], (int)r.c[1]};
+            if (D == 128 || (j4 & 1) == 0) scales[i][(rows0 + key) * (D / 32) + group] = (unsigned char)r.e;
+          }
+        }
       }
     }
     // A value that is NaN counts where its key is seen and nowhere else, and its weight may be zero where it is not: it goes
@@ -256,110 +451,88 @@ __global__ __launch_bounds__(64 * WAVES) void q4_attend_kernel(Q4Args a, TileDiv
     uint64_t bad[2];
 #pragma unroll
     for (int kt = 0; kt < 2; ++kt) {
-      bad[kt] = __builtin_amdgcn_ballot_w64(v[kt].e == 255u);
-      if (v[kt].e == 255u) {
-        v[kt].e = 127;
+      bad[kt] = __builtin_amdgcn_ballot_w64(u.v[kt].e == 255u);
+      if (u.v[kt].e == 255u) {
+        u.v[kt].e = 127;
 #pragma unroll
-        for (int t = 0; t < NT; ++t) v[kt].c[t] = 0;
+        for (int t = 0; t < NS; ++t) u.v[kt].c[t] = 0;
       }
-      const float unit = q4_unit_value(v[kt].e);
-      const int r = 16 * kt + qc;
-#pragma unroll
-      for (int t = 0; t < NT; ++t) *(bf16x8*)(vl + r * ROWB + (((j4 * NT + t) ^ swz<D>(r)) << 4)) = values(v[kt].c[t], unit);
     }
-    const int n = lim - key0 - 4 * j4;              // element (kt, e) is key key0 + 16 kt + 4 j4 + e
+    score(u);
 #pragma unroll
-    for (int kt = 0; kt < 2; ++kt)
+    for (int b = 0; b < RB; ++b) {
+      const int room = lim[b] - key0 - 4 * j4;      // element (kt, e) is key key0 + 16 kt + 4 j4 + e
 #pragma unroll
-      for (int e = 0; e < 4; ++e) s[kt][e] = 16 * kt + e < n ? s[kt][e] : -INFINITY;
-    const float tmax = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
-    const float mn = fmaxf(m, xor32_max(fmaxf(tmax, xor16(tmax)))), mm = mn == -INFINITY ? 0.f : mn;
-    const float alpha = __builtin_amdgcn_exp2f((m - mm) * c), neg = mm * -c;
-    m = mn;
-    l *= alpha;
+      for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt) o[dt] *= alpha;
-    bf16x8 p[PP];
-#pragma unroll
-    for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kt][e], c, neg));
-        l += y;
-        __bf16 part[PP];
-        split<PP>(y, part);
-#pragma unroll
-        for (int i = 0; i < PP; ++i) p[i][4 * kt + e] = part[i];
-      }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    const int rr = 4 * j4 + (qc >> 2);
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt) {
-      const unsigned at = lds0 + rr * ROWB + (((2 * dt + ((lane & 3) >> 1)) ^ swz<D>(rr)) << 4) + 8 * (lane & 1);
-      const s16x4 y0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4*)(size_t)at);
-      const unsigned at1 = lds0 + (rr + 16) * ROWB + (((2 * dt + ((lane & 3) >> 1)) ^ swz<D>(rr + 16)) << 4) + 8 * (lane & 1);
-      const s16x4 y1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4*)(size_t)at1);
-      const bf16x8 y = __builtin_shufflevector(__builtin_bit_cast(bf16x4, y0), __builtin_bit_cast(bf16x4, y1), 0, 1, 2, 3, 4, 5, 6, 7);
-#pragma unroll
-      for (int i = PP - 1; i >= 0; --i) o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(y, p[i], o[dt], 0, 0, 0);
+        for (int e = 0; e < 4; ++e) s[b][kt][e] = 16 * kt + e < room ? s[b][kt][e] : -INFINITY;
     }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
+    attend();
 #pragma unroll
     for (int kt = 0; kt < 2; ++kt)
-      for (uint64_t b = bad[kt]; b; b &= b - 1) {
-        const int at = __builtin_ctzll(b), key = key0 + 16 * kt + (at & 15);
-        if (key >= lim) continue;
+      for (uint64_t left = bad[kt]; left; left &= left - 1) {
+        const int at = __builtin_ctzll(left), key = key0 + 16 * kt + (at & 15);
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt)                  // lane at / 16 had columns D / 4 (at / 16) ..
-          if (dt / (DT / 4) == at >> 4) o[dt] = f32x4{NAN, NAN, NAN, NAN};
+        for (int b = 0; b < RB; ++b)
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt)                  // lane at / 16 had columns D / 4 (at / 16) ..
+            if (key < lim[b] && dt / (DT / 4) == at >> 4) st.o[b][dt] = f32x4{NAN, NAN, NAN, NAN};
       }
   }
 
   // the wavefronts meet, in a fixed order
-  l = xor32_sum(l + xor16(l));
-  if (j4 == 0) { lds_m[wave][qc] = m; lds_l[wave][qc] = l; }
+#pragma unroll
+  for (int b = 0; b < RB; ++b) {
+    const float l = xor32_sum(st.l[b] + xor16(st.l[b]));
+    if (j4 == 0) { lds_m[wave][16 * b + qc] = st.m[b]; lds_l[wave][16 * b + qc] = l; }
+  }
   __syncthreads();
-  float mt = -INFINITY, lt = 0.f;
-#pragma unroll
-  for (int k = 0; k < WAVES; ++k) mt = fmaxf(mt, lds_m[k][qc]);
-  const float mm = mt == -INFINITY ? 0.f : mt;
-#pragma unroll
-  for (int k = 0; k < WAVES; ++k) lt += lds_l[k][qc] * __builtin_amdgcn_exp2f((lds_m[k][qc] - mm) * c);
-  const float scale = lt == 0.f ? 0.f : __builtin_amdgcn_exp2f((m - mm) * c) * (1.f / lt);
-#pragma unroll
-  for (int dt = 0; dt < DT; ++dt) o[dt] *= scale;
   const size_t out0 = ((size_t)beta * a.plan.s_total + sp) * g.Hq * a.q_len;
-  if (threadIdx.x < 16 && live) a.LSE_sub[out0 + (size_t)head * a.q_len + j] = lt == 0.f ? -INFINITY : (mm * c + __builtin_amdgcn_logf(lt)) * LN2;
-  float* meet = (float*)lds_v[0];                     // [wave][16][D]: what V took, 16 rows of D floats a wavefront
-  static_assert(sizeof(lds_v[0]) == 16 * D * sizeof(float), "");
-  float* mine = meet + wave * 16 * D + qc * D;
-  __syncthreads();
+  float* meet = (float*)lds_v;                        // [wave][16][D]
 #pragma unroll
-  for (int dt = 0; dt < DT; ++dt) *(f32x4*)(mine + (((4 * dt + j4) ^ qc) & (D / 4 - 1)) * 4) = o[dt];
-  __syncthreads();
-  for (int i = threadIdx.x; i < 16 * (D / 4); i += 64 * WAVES) {
-    const int r = i / (D / 4), chunk = i % (D / 4), rw = tile * 16 + r;
-    if (rw >= R) break;
-    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  for (int b = 0; b < RB; ++b) {
+    float mt = -INFINITY, lt = 0.f;
 #pragma unroll
-    for (int k = 0; k < WAVES; ++k) acc += *(const f32x4*)(meet + k * 16 * D + r * D + ((chunk ^ r) & (D / 4 - 1)) * 4);
-    const int tj = (int)quotient(rw, by.G);
-    *(f32x4*)(a.O_sub + (out0 + (size_t)(kvh * g.G + rw - tj * g.G) * a.q_len + tj) * D + 4 * chunk) = acc;
+    for (int k = 0; k < WAVES; ++k) mt = fmaxf(mt, lds_m[k][16 * b + qc]);
+    const float mm = mt == -INFINITY ? 0.f : mt;
+#pragma unroll
+    for (int k = 0; k < WAVES; ++k) lt += lds_l[k][16 * b + qc] * __builtin_amdgcn_exp2f((lds_m[k][16 * b + qc] - mm) * c);
+    const float scale = lt == 0.f ? 0.f : __builtin_amdgcn_exp2f((st.m[b] - mm) * c) * (1.f / lt);
+    if (threadIdx.x < 16 && live[b])
+      a.LSE_sub[out0 + (size_t)head[b] * a.q_len + j[b]] = lt == 0.f ? -INFINITY : (mm * c + __builtin_amdgcn_logf(lt)) * LN2;
+    float* mine = meet + wave * 16 * D + qc * D;
+    if (b > 0) __syncthreads();
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) *(f32x4*)(mine + ((4 * dt + j4) ^ qc) * 4) = st.o[b][dt] * scale;
+    __syncthreads();
+    for (int i = threadIdx.x; i < 16 * (D / 4); i += 64 * WAVES) {
+      const int r = i / (D / 4), chunk = i % (D / 4), row = tile * 16 * RB + 16 * b + r;
+      if (row >= R) break;
+      f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int k = 0; k < WAVES; ++k) acc += *(const f32x4*)(meet + k * 16 * D + r * D + (chunk ^ r) * 4);
+      const int tj = (int)quotient(row, by.G);
+      *(f32x4*)(a.O_sub + (out0 + (size_t)(kvh * g.G + row - tj * g.G) * a.q_len + tj) * D + 4 * chunk) = acc;
+    }
   }
 }
 
-template <typename T, int D, int PP>
-hipError_t launch_attend(const Q4Args& a, hipStream_t st) {
+template <typename T, int D, int PP, int RB, bool NT>
+hipError_t launch_stream(const Q4Args& a, hipStream_t st) {
   const Geom& g = a.g;
-  const uint32_t tiles = (uint32_t)(((int64_t)g.G * a.q_len + 15) / 16);
-  const TileDiv by = {make_div(g.Hkv), make_div(tiles), make_div(a.plan.s_total), make_div(g.G)};
+  const uint32_t tiles = (uint32_t)(((int64_t)g.G * a.q_len + 16 * RB - 1) / (16 * RB));
+  const StreamDiv by = {make_div(g.Hkv), make_div(tiles), make_div(a.plan.s_total), make_div(g.G), make_div((uint32_t)a.plan.s_total * WAVES)};
   const int64_t wgs = (int64_t)g.B * g.Hkv * tiles * a.plan.s_total;
   if (wgs > 0x7fffffff) return hipErrorInvalidValue;
   return launch_in_pieces(wgs, 64 * WAVES, [&](unsigned first, unsigned n) {
-    q4_attend_kernel<T, D, PP><<<dim3(n), 64 * WAVES, 0, st>>>(a, by, first);
+    q4_stream_kernel<T, D, PP, RB, NT><<<dim3(n), 64 * WAVES, 0, st>>>(a, by, first);
   });
+}
+template <typename T, int D, int PP>
+hipError_t launch_stream(const Q4Args& a, hipStream_t st) {
+  const bool nt = !q4_cache_resident(a.g, a.cache_len);
+  if (a.plan.tile_rows == 16) return nt ? launch_stream<T, D, PP, 1, true>(a, st) : launch_stream<T, D, PP, 1, false>(a, st);
+  return nt ? launch_stream<T, D, PP, 2, true>(a, st) : launch_stream<T, D, PP, 2, false>(a, st);
 }
 
 }  // namespace
@@ -368,8 +541,8 @@ hipError_t launch_q4_store(int dtype, const Geom& g, const Q4Copy& c, hipStream_
 hipError_t launch_q4_load(int dtype, const Geom& g, const Q4Copy& c, hipStream_t st) { return launch_rows<true>(dtype, g, c, st); }
 
 hipError_t launch_phase2_q4(int dtype, const Q4Args& a, hipStream_t st) {
-  if (dtype != 0) return a.parts == 2 ? launch_attend<__bf16, 128, 2>(a, st) : launch_attend<__bf16, 128, 1>(a, st);
-  return a.g.d == 64 ? launch_attend<float, 64, 3>(a, st) : launch_attend<float, 128, 3>(a, st);
+  if (dtype != 0) return a.parts == 2 ? launch_stream<__bf16, 128, 2>(a, st) : launch_stream<__bf16, 128, 1>(a, st);
+  return a.g.d == 64 ? launch_stream<float, 64, 3>(a, st) : launch_stream<float, 128, 3>(a, st);
 }
 
 }  // namespace star

@@ -320,7 +320,12 @@ struct Q4Copy {
 hipError_t launch_q4_store(int dtype, const Geom& g, const Q4Copy& c, hipStream_t st);
 hipError_t launch_q4_load(int dtype, const Geom& g, const Q4Copy& c, hipStream_t st);
 
-// Phase 2 over a cache held in four bits, whose new rows have been filed: O_sub and LSE_sub of `plan`'s splits
+// Whether K and V in four bits, up to `keys`, are found in the 256 MB last-level cache by the next step (see decode_cache_resident).
+inline bool q4_cache_resident(const Geom& g, int64_t keys) {
+  return 2 * (int64_t)g.B * g.Hkv * keys * (g.d / 2 + g.d / 32) <= ((int64_t)192 << 20);
+}
+
+// Phase 2 over a cache held in four bits: O_sub and LSE_sub of `plan`'s splits.
 struct Q4Args {
   Geom g;
   SplitPlan plan;
@@ -328,11 +333,12 @@ struct Q4Args {
   int32_t q_len, causal;
   int32_t parts;          // bf16: bf16 parts a weight is taken in, 1 or 2
   const void* Qq;
+  const void* Kn;         // the call's K, V [B, q_len, Hkv, d], which the kernel files; null: the cache holds them, or there are none
+  const void* Vn;
   Q4Rows q4;
   float* O_sub;
   float* LSE_sub;
 };
-constexpr int Q4_TILE = 16;            // rows per tile
 hipError_t launch_phase2_q4(int dtype, const Q4Args& a, hipStream_t st);
 hipError_t launch_phase1_f32(const Phase1Args& a, hipStream_t st);
 hipError_t launch_phase2_f32(const Phase2Args& a, hipStream_t st);
