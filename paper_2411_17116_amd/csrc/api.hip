@@ -447,38 +447,68 @@ static bool make_plan(const star_attn_shape* s, int64_t q_len, int64_t total, bo
   return true;
 }
 
-// ---- four-bit cache: workgroups of 16 or 32 rows and a split
-constexpr int64_t Q4_WGS = 512;
-constexpr int64_t Q4_SPLIT_MIN = 128;      // keys: a unit of 32 for each of four wavefronts
-static int q4_tile(const Geom& g, int64_t q_len) { return (int64_t)g.G * q_len <= 16 ? 16 : 32; }
-static int64_t q4_splits(const Geom& g, int64_t q_len) {
-  const int64_t wgs = (int64_t)g.B * g.Hkv * ceil_div((int64_t)g.G * q_len, q4_tile(g, q_len));
-  return wgs < Q4_WGS ? Q4_WGS / wgs : 1;
+// ---- four-bit cache.  Few rows stream it (16 to a workgroup's tile, or 32 in bf16), two workgroups of four wavefronts on a CU; more are row-tiled (256 or
+// 128 in bf16, 128 or 64 in fp32), one workgroup of eight wavefronts on a CU, which share a tile's keys or, with the lower tile, take them in two halves.
+struct Q4Tiles {
+  int n, rows[2];
+};
+static Q4Tiles q4_tiles(const star_attn_shape* s, int64_t rows) {
+  const bool f32 = s->dtype == STAR_ATTN_F32;
+  if (rows <= 16) return {1, {16, 0}};
+  if (rows <= 32 && !f32) return {1, {32, 0}};
+  return f32 ? Q4Tiles{2, {128, 64}} : Q4Tiles{2, {256, 128}};
 }
-static bool make_q4_plan(const Geom& g, int64_t q_len, int64_t total, bool want_parts, SplitPlan* p) {
-  *p = SplitPlan{};
-  const int64_t n = ceil_div(g.L, g.b), want = q4_splits(g, q_len);
-  p->tile_rows = q4_tile(g, q_len);
-  p->n_blocks = (int32_t)n;
+// Splits of a row tile that the resident workgroups take at once, and the keys worth one.
+static int64_t q4_splits(const Geom& g, int64_t q_len, int tile) {
+  const int64_t wgs = (int64_t)g.B * g.Hkv * ceil_div((int64_t)g.G * q_len, tile), resident = tile <= 32 ? 512 : 256;
+  return wgs < resident ? resident / wgs : 1;
+}
+static int64_t q4_worth(int tile) { return tile <= 32 ? 128 : 256; }
+// Time of a row-tiled call, in hundredths of that of 64 keys: rounds of resident workgroups, each its keys and what it takes to start and to store; and
+// the per-split pairs.
+static double q4_cost(const Geom& g, int64_t q_len, int tile, bool low, int64_t splits, int64_t len) {
+  const double keys = low ? 110.0 * ceil_div(len, 128) : 100.0 * ceil_div(len, 64);
+  const int64_t wgs = splits * g.B * g.Hkv * ceil_div((int64_t)g.G * q_len, tile);
+  return ceil_div(wgs, 256) * (keys + 600) + 8.0 * splits * g.B * g.Hq * q_len * (g.d + 1) / 80000;
+}
+static bool make_q4_plan(const star_attn_shape* s, const Geom& g, int64_t q_len, int64_t total, bool want_parts, SplitPlan* p) {
+  const int64_t n = ceil_div(g.L, g.b), rows = (int64_t)g.G * q_len;
+  const Q4Tiles tiles = q4_tiles(s, rows);
   if (n > (1 << 24)) return false;
-  if (!want_parts) {
-    const int64_t worth = ceil_div(total, Q4_SPLIT_MIN), splits = want < worth ? want : worth;
-    p->flat = 1;
-    p->split_len = round_up(ceil_div(total, splits), 32);
-    p->s_total = (int32_t)ceil_div(total, p->split_len);
-    return true;
+  double least = 0;
+  bool found = false;
+  for (int i = 0; i < tiles.n; ++i) {
+    SplitPlan x = {};
+    const int tile = tiles.rows[i];
+    const int64_t want = q4_splits(g, q_len, tile), min_len = q4_worth(tile), unit = tile <= 32 ? 32 : 64;
+    x.tile_rows = tile;
+    x.decode = tile <= 32 ? 1 : 0;
+    x.n_blocks = (int32_t)n;
+    int64_t splits = 0;
+    if (!want_parts) {
+      const int64_t worth = ceil_div(total, min_len);
+      splits = want < worth ? want : worth;
+      x.flat = 1;
+      x.split_len = round_up(ceil_div(total, splits), unit);
+      splits = ceil_div(total, x.split_len);
+    } else {
+      const int64_t bmax = g.b < g.L ? g.b : g.L, most = bmax / min_len > 1 ? bmax / min_len : 1;
+      int64_t spb = ceil_div(want, n);
+      if (spb > most) spb = most;
+      x.split_len = round_up(ceil_div(bmax, spb), unit);
+      spb = ceil_div(bmax, x.split_len);
+      const int64_t st = g.cap > g.L ? ceil_div(g.cap - g.L, x.split_len) : 1;
+      splits = n * spb + st;
+      if (splits > (1 << 24)) continue;
+      x.spb = (int32_t)spb;
+      x.st = (int32_t)st;
+    }
+    x.s_total = (int32_t)splits;
+    const double cost = tiles.n == 1 ? 0 : q4_cost(g, q_len, tile, i == 1, splits, x.split_len);
+    if (!found || cost < least) { *p = x; least = cost; }
+    found = true;
   }
-  const int64_t bmax = g.b < g.L ? g.b : g.L, most = bmax / Q4_SPLIT_MIN > 1 ? bmax / Q4_SPLIT_MIN : 1;
-  int64_t spb = ceil_div(want, n);
-  if (spb > most) spb = most;
-  p->split_len = round_up(ceil_div(bmax, spb), 32);
-  spb = ceil_div(bmax, p->split_len);
-  const int64_t st = g.cap > g.L ? ceil_div(g.cap - g.L, p->split_len) : 1;
-  if (n * spb + st > (1 << 24)) return false;
-  p->spb = (int32_t)spb;
-  p->st = (int32_t)st;
-  p->s_total = (int32_t)(n * spb + st);
-  return true;
+  return found;
 }
 
 static size_t plan_bytes(const star_attn_shape* s, const SplitPlan& p, int64_t q_len) {
@@ -1013,7 +1043,7 @@ static int phase2_q4_impl(const star_attn_shape* shape, const star_attn_rotary* 
     return STAR_ATTN_ERR_MISALIGNED;
   const Geom g = make_geom(shape);
   SplitPlan plan;
-  if (!make_q4_plan(g, q_len, total, O_part != nullptr, &plan)) return STAR_ATTN_ERR_INVALID_SHAPE;
+  if (!make_q4_plan(shape, g, q_len, total, O_part != nullptr, &plan)) return STAR_ATTN_ERR_INVALID_SHAPE;
   if (workspace_bytes < plan_bytes(shape, plan, q_len)) return STAR_ATTN_ERR_WORKSPACE_TOO_SMALL;
   const int64_t rows = (int64_t)g.B * g.Hq * q_len;
   if (rows * plan.s_total > 0x7fffffff) return STAR_ATTN_ERR_INVALID_SHAPE;
@@ -1035,7 +1065,7 @@ static int phase2_q4_impl(const star_attn_shape* shape, const star_attn_rotary* 
   a.Vn = append && !rotary ? Vq : nullptr;
   a.O_sub = (float*)workspace;
   a.LSE_sub = (float*)workspace + rows * plan.s_total * g.d;
-  if (launch_phase2_q4(shape->dtype, a, st) != hipSuccess) return STAR_ATTN_ERR_LAUNCH_FAILED;
+  if ((plan.decode ? launch_phase2_q4_stream(shape->dtype, a, st) : launch_phase2_q4_tiles(shape->dtype, a, st)) != hipSuccess) return STAR_ATTN_ERR_LAUNCH_FAILED;
   MergeArgs m;
   m.g = g; m.plan = plan; m.wide = 0; m.keep_nan = 1;
   m.q_len = (int32_t)q_len; m.out_bf16 = shape->dtype == STAR_ATTN_BF16;
@@ -1065,22 +1095,31 @@ size_t star_attn_q4_workspace_bytes(const star_attn_shape* shape, int64_t max_q_
   if (validate_shape(shape) != STAR_ATTN_OK || max_q_len <= 0) return 0;
   const Geom g = make_geom(shape);
   size_t best = 0;
-  // A call's splits go by how many the resident workgroups leave for its rows, and by the cache: the longest call of each such number.
-  auto consider = [&](int64_t q) {
-    SplitPlan p;
-    if (make_q4_plan(g, q, g.cap, true, &p) && plan_bytes(shape, p, q) > best) best = plan_bytes(shape, p, q);
-    // (equal runs of a shorter cache may be more than the whole cache's, whose length is rounded up)
-    const int64_t want = q4_splits(g, q), worth = ceil_div(g.cap, Q4_SPLIT_MIN);
+  // A call has at most as many equal runs as its tile's resident workgroups leave for it, or as many splits of every part: the longest call of each
+  // such number, for every tile that a call may take.
+  const auto need = [&](int64_t q, int tile) {
+    SplitPlan p = {};
+    const int64_t want = q4_splits(g, q, tile), worth = ceil_div(g.cap, q4_worth(tile));
     p.s_total = (int32_t)(want < worth ? want : worth);
     if (plan_bytes(shape, p, q) > best) best = plan_bytes(shape, p, q);
   };
+  const auto consider = [&](int64_t q) {
+    if (q < 1) return;
+    if (q > max_q_len) q = max_q_len;
+    const Q4Tiles tiles = q4_tiles(shape, (int64_t)g.G * q);
+    for (int i = 0; i < tiles.n; ++i) need(q, tiles.rows[i]);
+    SplitPlan p;
+    if (make_q4_plan(shape, g, q, g.cap, true, &p) && plan_bytes(shape, p, q) > best) best = plan_bytes(shape, p, q);
+  };
   const int64_t pairs = (int64_t)g.B * g.Hkv;
-  for (int64_t want = 1; want * pairs <= Q4_WGS; ++want) {
-    for (int tile = 16; tile <= 32; tile += 16) {
-      const int64_t q = (tile == 16 ? 1 : Q4_WGS / (pairs * want)) * tile / g.G;
-      if (q >= 1) consider(q < max_q_len ? q : max_q_len);
+  for (int tile = 16; tile <= 256; tile *= 2)
+    for (int64_t want = 1; want * pairs <= 512; ++want) {
+      const int64_t q = 512 / (pairs * want) * tile / g.G, half = 256 / (pairs * want) * tile / g.G;
+      consider(tile == 16 && q > 16 / g.G ? 16 / g.G : q);
+      consider(tile == 32 && half > 32 / g.G ? 32 / g.G : half);
     }
-  }
+  consider(16 / g.G);
+  consider(32 / g.G);
   consider(max_q_len);
   return best;
 }
@@ -1107,8 +1146,10 @@ int star_attn_phase2_q4_plan(const star_attn_shape* shape, int64_t cache_len, in
   if (q_len <= 0 || q_len > (1 << 20) || cache_len < shape->ctx_len) return STAR_ATTN_ERR_INVALID_SHAPE;
   if (cache_len + q_len > shape->cache_capacity) return STAR_ATTN_ERR_CACHE_OVERFLOW;
   SplitPlan plan;
-  if (!make_q4_plan(make_geom(shape), q_len, cache_len + q_len, want_parts != 0, &plan)) return STAR_ATTN_ERR_INVALID_SHAPE;
+  if (!make_q4_plan(shape, make_geom(shape), q_len, cache_len + q_len, want_parts != 0, &plan)) return STAR_ATTN_ERR_INVALID_SHAPE;
   *out = star_attn_plan_info{};
+  out->decode = plan.decode;
+  out->non_temporal = plan.decode && !q4_cache_resident(make_geom(shape), cache_len) ? 1 : 0;
   out->flat = plan.flat;
   out->n_splits = plan.s_total;
   out->tile_rows = plan.tile_rows;

@@ -1,21 +1,10 @@
 // A cache held in four bits: rows filed into it and read from it, and phase 2 over it (Eq. 1-2 per split of the cache; the
 // merge kernels fold the splits, Eq. 3-4).  q4.h says what a row is.
-#include "q4.h"
+#include "q4_attend.h"
 
 namespace star {
 
 namespace {
-
-typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
-typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
-typedef __attribute__((ext_vector_type(4))) float f32x4;
-typedef __attribute__((ext_vector_type(4))) short s16x4;
-typedef __attribute__((ext_vector_type(4))) int i32x4;
-
-#define LDS_AS __attribute__((address_space(3)))
-
-constexpr float LOG2E = 1.4426950408889634f;
-constexpr float LN2 = 0.6931471805599453f;
 
 // ------------------------------------------------------------------ rows filed and read
 // Bound by HBM: a lane has eight elements of K and then of V, four lanes a group.
@@ -26,18 +15,6 @@ struct CopyArgs {
   uint32_t total;         // (batch, head, row)
 };
 
-template <typename T>
-__device__ __forceinline__ void load8(const T* p, float (&x)[8]) {
-  if constexpr (sizeof(T) == 2) {
-    const bf16x8 v = *(const bf16x8*)p;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = (float)v[e];
-  } else {
-    const f32x4 v = *(const f32x4*)p, w = *(const f32x4*)(p + 4);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) { x[e] = v[e]; x[4 + e] = w[e]; }
-  }
-}
 template <typename T>
 __device__ __forceinline__ void store8(T* p, const float (&x)[8]) {
   if constexpr (sizeof(T) == 2) {
@@ -122,20 +99,6 @@ hipError_t launch_rows(int dtype, const Geom& g, const Q4Copy& c, hipStream_t st
 //     queries of different sizes.)  The exponentiated unit is the B operand of O^T += V^T P^T, weights in PP bf16 parts, V by way of LDS to be read back transposed.
 //   * The call's own keys are put into four bits by the wavefront whose unit has them, which files them and attends to them from its registers.
 
-// chunk c (16 bytes) of V's row r sits in slot c ^ (r & 7): eight rows' chunk, which eight lanes write at once, lie in eight different ones, as do
-// the two chunks of four rows that a transposing read of sixteen lanes takes with its neighbours'
-__device__ __forceinline__ int swz(int r) { return r & 7; }
-
-__device__ __forceinline__ float xor16(float x) { return __int_as_float(__builtin_amdgcn_ds_swizzle(__float_as_int(x), 0x401F)); }
-__device__ __forceinline__ float xor32_max(float x) {
-  auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-}
-__device__ __forceinline__ float xor32_sum(float x) {
-  auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
-
 constexpr int WAVES = 4;
 constexpr int UNIT = 32;              // keys a wavefront takes at once
 
@@ -156,7 +119,6 @@ __device__ __forceinline__ V fetch(GlobalBytes p) {
   const __attribute__((address_space(1))) V* q = (const __attribute__((address_space(1))) V*)p;
   return NT ? __builtin_nontemporal_load(q) : *q;
 }
-typedef __attribute__((ext_vector_type(2))) int i32x2;
 // (codes and exponents of the lane's key; codes' rows are D / 2 bytes, exponents' D / 32)
 template <int D, bool NT>
 __device__ __forceinline__ void load_rows(Rows16<D>& x, GlobalBytes codes, GlobalBytes scales) {
@@ -171,36 +133,12 @@ __device__ __forceinline__ void load_rows(Rows16<D>& x, GlobalBytes codes, Globa
   }
   x.e = fetch<unsigned char, NT>(scales);
 }
-__device__ __forceinline__ bf16x8 values(uint32_t c, float unit) {
-  const q4_bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, unit, 0), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, unit, 1);
-  const q4_bf16x2 x = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, unit, 2), y = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, unit, 3);
-  return bf16x8{a[0], a[1], b[0], b[1], x[0], x[1], y[0], y[1]};
-}
-
-// x = p[0] + p[1] + .. in bf16 parts.  Three hold 24 bits and are cut off, so that none overflows; an infinity or NaN is the
-// first's alone.
-template <int P>
-__device__ __forceinline__ void split(float x, __bf16 (&p)[P]) {
-  if constexpr (P == 3) {
-    const bool finite = magnitude_bits(x) < 0x7f800000u;
-    float r = x;
-#pragma unroll
-    for (int i = 0; i < 3; ++i) {
-      const float y = __uint_as_float(__float_as_uint(r) & 0xffff0000u);
-      p[i] = i == 0 && !finite ? (__bf16)x : (__bf16)y;
-      r = finite ? r - y : 0.f;
-    }
-  } else {
-    p[0] = (__bf16)x;
-    if constexpr (P == 2) p[1] = (__bf16)(x - (float)p[0]);
-  }
-}
-
 template <int QP, int NT, int DT, int RB>
 struct StreamState {
   bf16x8 q[RB][QP][NT];   // Q^T fragments: D / 4 (lane / 16) + 8 t ..+7 of row lane % 16
   f32x4 o[RB][DT];        // O^T: element 16 dt + 4 (lane / 16) + v of that row
-  float m[RB], l[RB], neg[RB];      // running maximum of the logits, this lane's share of the sum, -m c (0 while nothing was visible)
+  float m[RB], l[RB], neg[RB], above[RB];      // running maximum of the logits, this lane's share of the sum, -m c (0 while nothing was visible), the exponent
+                          // that moves the maximum
 };
 
 struct StreamDiv {
@@ -208,7 +146,7 @@ struct StreamDiv {
 };
 
 template <typename T, int D, int PP, int RB, bool NT>
-__global__ __launch_bounds__(64 * WAVES, RB == 1 && sizeof(T) == 2 ? 3 : 2) void q4_stream_kernel(Q4Args a, StreamDiv by, unsigned first_wg) {
+__global__ __launch_bounds__(64 * WAVES, 2) void q4_stream_kernel(Q4Args a, StreamDiv by, unsigned first_wg) {
   constexpr int QP = sizeof(T) == 2 ? 1 : 3, NS = D / 32, DT = D / 16, ROWB = 2 * D;
   __shared__ __attribute__((aligned(1024))) char lds_v[WAVES][UNIT * ROWB];      // 16 rows of D floats of a wavefront, too
   __shared__ float lds_m[WAVES][16 * RB], lds_l[WAVES][16 * RB];
@@ -290,19 +228,19 @@ __global__ __launch_bounds__(64 * WAVES, RB == 1 && sizeof(T) == 2 ? 3 : 2) void
     }
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) st.o[b][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
-    st.m[b] = -INFINITY;
+    st.m[b] = st.above[b] = -INFINITY;
     st.l[b] = st.neg[b] = 0.f;
   }
   const float c = g.scale * LOG2E;
   char* vl = lds_v[wave];
   const unsigned lds0 = (unsigned)(size_t)(LDS_AS char*)vl;
-  unsigned vw[NS];                      // (row qc of the first 16; the others' are 16 rows further, 16 being 0 modulo 8)
+  unsigned vw[NS];                      // (row qc of the first 16; the others' are 16 rows further)
 #pragma unroll
-  for (int t = 0; t < NS; ++t) vw[t] = lds0 + qc * ROWB + (((j4 * NS + t) ^ swz(qc)) << 4);
+  for (int t = 0; t < NS; ++t) vw[t] = lds0 + qc * ROWB + (((j4 * NS + t) ^ swz<D>(qc)) << 4);
   const int rr = 4 * j4 + (qc >> 2);
   unsigned vr[DT];
 #pragma unroll
-  for (int dt = 0; dt < DT; ++dt) vr[dt] = lds0 + rr * ROWB + (((2 * dt + ((lane & 3) >> 1)) ^ swz(rr)) << 4) + 8 * (lane & 1);
+  for (int dt = 0; dt < DT; ++dt) vr[dt] = lds0 + rr * ROWB + (((2 * dt + ((lane & 3) >> 1)) ^ swz<D>(rr)) << 4) + 8 * (lane & 1);
 
   // A unit's scores, and V into LDS: its registers are then free.
   f32x4 s[RB][2];
@@ -343,30 +281,27 @@ __global__ __launch_bounds__(64 * WAVES, RB == 1 && sizeof(T) == 2 ? 3 : 2) void
     bf16x8 p[RB][PP];
 #pragma unroll
     for (int b = 0; b < RB; ++b) {
-      const float tmax = fmaxf(fmaxf(fmaxf(s[b][0][0], s[b][0][1]), fmaxf(s[b][0][2], s[b][0][3])),
-                               fmaxf(fmaxf(s[b][1][0], s[b][1][1]), fmaxf(s[b][1][2], s[b][1][3])));
+      Exponents t = exponents(s[b], c, st.neg[b]);
       // lanes exchange their maxima only where some row's moves
-      if (__builtin_amdgcn_ballot_w64(tmax > st.m[b]) != 0) {
-        const float m = fmaxf(st.m[b], xor32_max(fmaxf(tmax, xor16(tmax)))), mm = m == -INFINITY ? 0.f : m;
+      if (__builtin_amdgcn_ballot_w64(largest(t) > st.above[b]) != 0) {
+        const float m = fmaxf(st.m[b], quad_max(largest(exponents(s[b], 1.f, 0.f)))), mm = m == -INFINITY ? 0.f : m;
         const float alpha = __builtin_amdgcn_exp2f((st.m[b] - mm) * c);
         st.l[b] *= alpha;
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) st.o[b][dt] *= alpha;
         st.m[b] = m;
         st.neg[b] = mm * -c;
+        st.above[b] = m == -INFINITY ? -INFINITY : 0.f;
+        t = exponents(s[b], c, st.neg[b]);
       }
       float sum = 0.f;
 #pragma unroll
-      for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][kt][e], c, st.neg[b]));
-          sum += y;
-          __bf16 part[PP];
-          split<PP>(y, part);
-#pragma unroll
-          for (int i = 0; i < PP; ++i) p[b][i][4 * kt + e] = part[i];
-        }
+      for (int i = 0; i < 8; i += 2) {
+        const float y = __builtin_amdgcn_exp2f(t.x[i]), z = __builtin_amdgcn_exp2f(t.x[i + 1]);
+        sum += y;
+        sum += z;
+        split_pair<PP>(y, z, p[b], i);
+      }
       st.l[b] += sum;
     }
 #pragma unroll
@@ -483,7 +418,7 @@ __global__ __launch_bounds__(64 * WAVES, RB == 1 && sizeof(T) == 2 ? 3 : 2) void
   // the wavefronts meet, in a fixed order
 #pragma unroll
   for (int b = 0; b < RB; ++b) {
-    const float l = xor32_sum(st.l[b] + xor16(st.l[b]));
+    const float l = quad_sum(st.l[b]);
     if (j4 == 0) { lds_m[wave][16 * b + qc] = st.m[b]; lds_l[wave][16 * b + qc] = l; }
   }
   __syncthreads();
@@ -528,11 +463,9 @@ hipError_t launch_stream(const Q4Args& a, hipStream_t st) {
     q4_stream_kernel<T, D, PP, RB, NT><<<dim3(n), 64 * WAVES, 0, st>>>(a, by, first);
   });
 }
-template <typename T, int D, int PP>
+template <typename T, int D, int PP, int RB>
 hipError_t launch_stream(const Q4Args& a, hipStream_t st) {
-  const bool nt = !q4_cache_resident(a.g, a.cache_len);
-  if (a.plan.tile_rows == 16) return nt ? launch_stream<T, D, PP, 1, true>(a, st) : launch_stream<T, D, PP, 1, false>(a, st);
-  return nt ? launch_stream<T, D, PP, 2, true>(a, st) : launch_stream<T, D, PP, 2, false>(a, st);
+  return q4_cache_resident(a.g, a.cache_len) ? launch_stream<T, D, PP, RB, false>(a, st) : launch_stream<T, D, PP, RB, true>(a, st);
 }
 
 }  // namespace
@@ -540,9 +473,15 @@ hipError_t launch_stream(const Q4Args& a, hipStream_t st) {
 hipError_t launch_q4_store(int dtype, const Geom& g, const Q4Copy& c, hipStream_t st) { return launch_rows<false>(dtype, g, c, st); }
 hipError_t launch_q4_load(int dtype, const Geom& g, const Q4Copy& c, hipStream_t st) { return launch_rows<true>(dtype, g, c, st); }
 
-hipError_t launch_phase2_q4(int dtype, const Q4Args& a, hipStream_t st) {
-  if (dtype != 0) return a.parts == 2 ? launch_stream<__bf16, 128, 2>(a, st) : launch_stream<__bf16, 128, 1>(a, st);
-  return a.g.d == 64 ? launch_stream<float, 64, 3>(a, st) : launch_stream<float, 128, 3>(a, st);
+hipError_t launch_phase2_q4_stream(int dtype, const Q4Args& a, hipStream_t st) {
+  const int64_t rows = (int64_t)a.g.G * a.q_len;
+  if (rows > a.plan.tile_rows || a.plan.tile_rows != (rows <= 16 ? 16 : 32)) return hipErrorInvalidValue;
+  if (dtype == 0) {
+    if (rows > 16) return hipErrorInvalidValue;
+    return a.g.d == 64 ? launch_stream<float, 64, 3, 1>(a, st) : launch_stream<float, 128, 3, 1>(a, st);
+  }
+  if (rows <= 16) return a.parts == 2 ? launch_stream<__bf16, 128, 2, 1>(a, st) : launch_stream<__bf16, 128, 1, 1>(a, st);
+  return a.parts == 2 ? launch_stream<__bf16, 128, 2, 2>(a, st) : launch_stream<__bf16, 128, 1, 2>(a, st);
 }
 
 }  // namespace star

@@ -1,0 +1,124 @@
+// What the kernels that attend to a cache in four bits share.
+#pragma once
+
+#include "q4.h"
+
+namespace star {
+namespace {
+
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(4))) short s16x4;
+typedef __attribute__((ext_vector_type(4))) int i32x4;
+typedef __attribute__((ext_vector_type(2))) int i32x2;
+
+#define LDS_AS __attribute__((address_space(3)))
+
+constexpr float LOG2E = 1.4426950408889634f;
+constexpr float LN2 = 0.6931471805599453f;
+
+// Eight elements of a plain row.
+template <typename T>
+__device__ __forceinline__ void load8(const T* p, float (&x)[8]) {
+  if constexpr (sizeof(T) == 2) {
+    const bf16x8 v = *(const bf16x8*)p;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = (float)v[e];
+  } else {
+    const f32x4 v = *(const f32x4*)p, w = *(const f32x4*)(p + 4);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) { x[e] = v[e]; x[4 + e] = w[e]; }
+  }
+}
+
+// Eight codes times their unit.
+__device__ __forceinline__ bf16x8 values(uint32_t c, float unit) {
+  const q4_bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, unit, 0), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, unit, 1);
+  const q4_bf16x2 x = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, unit, 2), y = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, unit, 3);
+  return bf16x8{a[0], a[1], b[0], b[1], x[0], x[1], y[0], y[1]};
+}
+
+// x = p[0] + p[1] + .. in bf16 parts.  Three hold 24 bits and are cut off, so that none overflows; an infinity or NaN is the
+// first's alone.
+template <int P>
+__device__ __forceinline__ void split(float x, __bf16 (&p)[P]) {
+  if constexpr (P == 3) {
+    const bool finite = magnitude_bits(x) < 0x7f800000u;
+    float r = x;
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+      const float y = __uint_as_float(__float_as_uint(r) & 0xffff0000u);
+      p[i] = i == 0 && !finite ? (__bf16)x : (__bf16)y;
+      r = finite ? r - y : 0.f;
+    }
+  } else {
+    p[0] = (__bf16)x;
+    if constexpr (P == 2) p[1] = (__bf16)(x - (float)p[0]);
+  }
+}
+
+// Exponents of eight weights (as powers of two) against a reference, and the largest of them; NaN are passed over.
+struct Exponents {
+  float x[8];
+};
+__device__ __forceinline__ Exponents exponents(const f32x4 (&s)[2], float c, float neg) {
+  Exponents t;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) t.x[i] = __builtin_fmaf(s[i >> 2][i & 3], c, neg);
+  return t;
+}
+__device__ __forceinline__ float largest(const Exponents& t) {
+  return fmaxf(fmaxf(fmaxf(fmaxf(t.x[0], t.x[1]), t.x[2]), fmaxf(fmaxf(t.x[3], t.x[4]), t.x[5])), fmaxf(t.x[6], t.x[7]));
+}
+
+// Two weights in PP bf16 parts, slots e and e + 1 of the operands.
+template <int PP>
+__device__ __forceinline__ void split_pair(float x, float y, bf16x8 (&p)[PP], int e) {
+  if constexpr (PP == 3) {
+    float a = x, b = y;
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {          // (cut off: weights are at most 2^8, and no part overflows)
+      const uint32_t u = __float_as_uint(a) & 0xffff0000u, v = __float_as_uint(b) & 0xffff0000u;
+      const bf16x2 z = __builtin_bit_cast(bf16x2, i < 2 ? (u >> 16) | v : (__float_as_uint(a) >> 16) | v);
+      p[i][e] = z[0];
+      p[i][e + 1] = z[1];
+      a -= __uint_as_float(u);
+      b -= __uint_as_float(v);
+    }
+  } else {
+    const bf16x2 z = {(__bf16)x, (__bf16)y};
+    p[0][e] = z[0];
+    p[0][e + 1] = z[1];
+    if constexpr (PP == 2) {
+      const uint32_t u = __builtin_bit_cast(uint32_t, z);
+      const bf16x2 w = {(__bf16)(x - __uint_as_float(u << 16)), (__bf16)(y - __uint_as_float(u & 0xffff0000u))};
+      p[1][e] = w[0];
+      p[1][e + 1] = w[1];
+    }
+  }
+}
+
+// Chunk c (16 bytes) of row r in LDS sits in slot c ^ swz(r).  What a wavefront reads or writes at once is chunk c + D / 32 (lane / 16) of row lane % 16 or, transposing, two
+// chunks of each row; with the row's bits rotated (of 128-byte rows, two to a line, without the lowest) neither meets itself in a bank.
+template <int D>
+__device__ __forceinline__ int swz(int r) {
+  return D == 128 ? ((r << 1) & 15) | ((r >> 3) & 1) : ((r & 6) | ((r >> 3) & 1));
+}
+
+// The four lanes l, l ^ 16, l ^ 32, l ^ 48 hold the keys of one row.
+__device__ __forceinline__ float xor16(float x) { return __int_as_float(__builtin_amdgcn_ds_swizzle(__float_as_int(x), 0x401F)); }
+__device__ __forceinline__ float quad_max(float x) {
+  x = fmaxf(x, xor16(x));
+  auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float quad_sum(float x) {
+  x += xor16(x);
+  auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+}  // namespace
+}  // namespace star

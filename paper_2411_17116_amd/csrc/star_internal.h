@@ -339,7 +339,8 @@ struct Q4Args {
   float* O_sub;
   float* LSE_sub;
 };
-hipError_t launch_phase2_q4(int dtype, const Q4Args& a, hipStream_t st);
+hipError_t launch_phase2_q4_stream(int dtype, const Q4Args& a, hipStream_t st);      // plan.decode
+hipError_t launch_phase2_q4_tiles(int dtype, const Q4Args& a, hipStream_t st);
 hipError_t launch_phase1_f32(const Phase1Args& a, hipStream_t st);
 hipError_t launch_phase2_f32(const Phase2Args& a, hipStream_t st);
 hipError_t launch_phase1_bf16(const Phase1Args& a, hipStream_t st);
