@@ -408,7 +408,7 @@ int star_attn_phase2_norm_rope(const star_attn_shape* shape, const star_attn_rot
  * waits for, or what does not fit.
  *
  * A row of d elements is d / 32 groups.  A group is 32 codes and one exponent byte e, its
- * unit 2^(e - 127): the largest power of two u with 3.5 u <= max |x|, from 2^-125 to 2^125.  A code
+ * unit 2^(e - 127): the largest power of two u with 3.5 u <= max |x|, from 2^-125 to 2^125 (one for a group of zeros).  A code
  * stands for its sign (bit 3) times 0, .5, 1, 1.5, 2, 3, 4, 6 (bits 0 to 2) units, and is
  * the nearest of these to the element (the even code of two as near): off by a quarter of a unit for
  * small elements and by at most one, a fifth of the group's largest element, between 4 and 7 units.

@@ -22,6 +22,7 @@ def quantise(x):
         up = fine & (e < 252) & (3.5 * unit[(e + 1).long()] <= most)
         down = fine & (e > 2) & (3.5 * unit[e.long()] > most)
         e = e + up.double() - down.double()
+    e[fine & (most == 0)] = 127
     y = g.abs() / unit[e.long()][..., None]
     y = torch.where(fine[..., None], y, torch.zeros_like(y))
     off = (y[..., None] - GRID.to(x.device)).abs()
@@ -48,7 +49,8 @@ def values(codes, exponents):
 
 def attend(Q, K, V, scale, cache_len=None, lo=0, hi=None):
     """Q [q, d] of one head against rows [lo, hi) of K, V [n, d], new token j seeing rows up to cache_len + j (None: all).
-    Returns A [q, d], lse [q], and what error bounds are made of: sum p |v| [q, d], the largest sum |q k| scale of a row [q]."""
+    Returns A [q, d], lse [q], and what error bounds are made of: sum p |v| [q, d], the largest sum |q k| scale of a row [q], and
+    the sum of |v| over the seen keys whose values fp16 holds [q, d]."""
     Q, K, V = Q.double(), K.double(), V.double()
     hi = K.shape[0] if hi is None else hi
     seen = torch.zeros(Q.shape[0], K.shape[0], dtype=torch.bool, device=Q.device)
@@ -62,7 +64,8 @@ def attend(Q, K, V, scale, cache_len=None, lo=0, hi=None):
     if torch.isfinite(V).all():
         pick = lambda X: p @ X
     size = torch.where(seen, Q.abs() @ K.abs().T * scale, torch.zeros_like(s)).amax(-1)
-    return pick(V), lse, pick(V.abs()), size
+    held = torch.where(V.abs() <= 6 * 2.0 ** 13, V.abs(), torch.zeros_like(V))
+    return pick(V), lse, pick(V.abs()), size, seen.double() @ held
 
 
 def norm_rope(x, weight, eps, theta, positions, axis):

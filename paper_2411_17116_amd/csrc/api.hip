@@ -1059,7 +1059,7 @@ static int phase2_q4_impl(const star_attn_shape* shape, const star_attn_rotary* 
   }
   Q4Args a;
   a.g = g; a.plan = plan; a.cache_len = cache_len; a.q_len = (int32_t)q_len; a.causal = append ? 1 : 0;
-  a.parts = pair || O_part ? 2 : 1;        // (weights in bf16 are what bf16 outputs show; fp32 ones are held to more)
+  a.parts = pair || O_part ? 2 : 1;        // (a weight rounded to 11 bits does not show in bf16 outputs; fp32 ones are held to more)
   a.Qq = Qq; a.q4 = q4;
   a.Kn = append && !rotary ? Kq : nullptr;
   a.Vn = append && !rotary ? Vq : nullptr;

@@ -2,7 +2,7 @@
 // 0, .5, 1, 1.5, 2, 3, 4, 6) and the exponent byte e of its unit 2^(e - 127).  The unit is the largest power of two u with 3.5 u <=
 // max |x|, so that the largest element is 3.5 to 7 units and its code 4 or 6.  255 marks a group that holds a NaN or an infinity, which four bits cannot tell apart: it reads as NaN.
 // Units stay within 2^-125 and 2^125, where every value a code stands for is a normal bf16 and fp32 number: values are exact in
-// either type, and a group whose largest element is below 2^-126 reads as zeros (or half a unit).
+// either type, and a group whose largest element is below 2^-126 reads as zeros (or half a unit).  A group of zeros has the unit one.
 // Codes and units are what gfx950's conversions take, so a pair of elements costs one instruction either way.
 #pragma once
 
@@ -17,6 +17,7 @@ typedef __attribute__((ext_vector_type(2))) float q4_f32x2;
 // values, NaN above infinity above all).
 __device__ __forceinline__ uint32_t q4_unit(uint32_t most) {
   if (most >= 0x7f800000u) return 255u;
+  if (most == 0u) return 127u;
   const int e = (int)((most + 0x200000u) >> 23) - 2;         // (a mantissa of 1.75 and more: the next power of two)
   return (uint32_t)(e < 2 ? 2 : e > 252 ? 252 : e);
 }

@@ -2,6 +2,8 @@
 // merge kernels fold the splits, Eq. 3-4).  q4.h says what a row is.
 #include "q4_attend.h"
 
+#include <type_traits>
+
 namespace star {
 
 namespace {
@@ -96,7 +98,7 @@ hipError_t launch_rows(int dtype, const Geom& g, const Q4Copy& c, hipStream_t st
 //     K; two units are in registers, and a unit's are requested again as soon as its K is multiplied and its V in LDS.
 //   * S^T = K Q^T in bf16 products, which lose nothing: a four-bit value is a bf16 number, an fp32 query three of them.  (The instruction that
 //     multiplies four-bit codes as they are, by queries in two 8-bit parts, adds up a group's products in fewer bits: 2^-11 of sum |q k| off with
-//     queries of different sizes.)  The exponentiated unit is the B operand of O^T += V^T P^T, weights in PP bf16 parts, V by way of LDS to be read back transposed.
+//     queries of different sizes.)  The exponentiated unit is the B operand of O^T += V^T P^T, weights in PP parts (q4_attend.h), V by way of LDS to be read back transposed.
 //   * The call's own keys are put into four bits by the wavefront whose unit has them, which files them and attends to them from its registers.
 
 constexpr int WAVES = 4;
@@ -137,7 +139,7 @@ template <int QP, int NT, int DT, int RB>
 struct StreamState {
   bf16x8 q[RB][QP][NT];   // Q^T fragments: D / 4 (lane / 16) + 8 t ..+7 of row lane % 16
   f32x4 o[RB][DT];        // O^T: element 16 dt + 4 (lane / 16) + v of that row
-  float m[RB], l[RB], neg[RB], above[RB];      // running maximum of the logits, this lane's share of the sum, -m c (0 while nothing was visible), the exponent
+  float m[RB], l[RB], neg[RB], above[RB];      // running maximum of the logits, this lane's share of the sum, TOP - m c (0 while nothing was visible), the exponent
                           // that moves the maximum
 };
 
@@ -198,7 +200,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void q4_stream_kernel(Q4Args a, Stre
   GlobalBytes vc = (GlobalBytes)a.q4.v_codes + rows0 * (D / 2), vs = (GlobalBytes)a.q4.v_scales + rows0 * (D / 32);
   const int group = D == 128 ? j4 : j4 >> 1;
   const unsigned c_off = qc * (D / 2) + j4 * (D / 8), s_off = qc * (D / 32) + group;
-  const auto load_whole = [&](UnitRegs<D>& u, int s) {
+  const auto load_whole = [&](UnitRegs<D>& u, int s) INLINE {
     const int key0 = base + s * stride;
     GlobalBytes a0 = kc + (size_t)key0 * (D / 2), a1 = ks + (size_t)key0 * (D / 32), a2 = vc + (size_t)key0 * (D / 2), a3 = vs + (size_t)key0 * (D / 32);
 #pragma unroll
@@ -207,9 +209,6 @@ __global__ __launch_bounds__(64 * WAVES, 2) void q4_stream_kernel(Q4Args a, Stre
     for (int kt = 0; kt < 2; ++kt) load_rows<D, NT>(u.v[kt], a2 + kt * 16 * (D / 2) + c_off, a3 + kt * 16 * (D / 32) + s_off);
   };
 
-  UnitRegs<D> u0, u1;
-  if (0 < n_whole) load_whole(u0, 0);
-  if (1 < n_whole) load_whole(u1, 1);
   StreamState<QP, NS, DT, RB> st;
 #pragma unroll
   for (int b = 0; b < RB; ++b) {
@@ -221,15 +220,11 @@ __global__ __launch_bounds__(64 * WAVES, 2) void q4_stream_kernel(Q4Args a, Stre
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         __bf16 part[QP];
-        split<QP>(live[b] ? y[e] : 0.f, part);
+        split(live[b] ? y[e] : 0.f, part);
 #pragma unroll
         for (int i = 0; i < QP; ++i) st.q[b][i][t][e] = part[i];
       }
     }
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt) st.o[b][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
-    st.m[b] = st.above[b] = -INFINITY;
-    st.l[b] = st.neg[b] = 0.f;
   }
   const float c = g.scale * LOG2E;
   char* vl = lds_v[wave];
@@ -242,179 +237,210 @@ __global__ __launch_bounds__(64 * WAVES, 2) void q4_stream_kernel(Q4Args a, Stre
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt) vr[dt] = lds0 + rr * ROWB + (((2 * dt + ((lane & 3) >> 1)) ^ swz<D>(rr)) << 4) + 8 * (lane & 1);
 
-  // A unit's scores, and V into LDS: its registers are then free.
-  f32x4 s[RB][2];
-  const auto score = [&](const UnitRegs<D>& u) {
+  Wide wide = {0, 0};
+  int down = 0;
+  const auto walk = [&](auto WIDE) INLINE {
+    typedef Product<WIDE.value> P;
+    typedef typename P::Vec Vec;
+    constexpr int PARTS = WIDE.value && PP > 1 ? 3 : PP;
+    UnitRegs<D> u0, u1;
+    if (0 < n_whole) load_whole(u0, 0);
+    if (1 < n_whole) load_whole(u1, 1);
 #pragma unroll
-    for (int kt = 0; kt < 2; ++kt) {
-      const float unit = q4_unit_value(u.k[kt].e);
+    for (int b = 0; b < RB; ++b) {
 #pragma unroll
-      for (int t = 0; t < NS; ++t) {
-        const bf16x8 y = values(u.k[kt].c[t], unit);
+      for (int dt = 0; dt < DT; ++dt) st.o[b][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+      st.m[b] = st.above[b] = -INFINITY;
+      st.l[b] = st.neg[b] = 0.f;
+    }
+    // A unit's scores, and V into LDS: its registers are then free.
+    f32x4 s[RB][2];
+    const auto score = [&](const UnitRegs<D>& u) INLINE {
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt) {
+        const float unit = q4_unit_value(u.k[kt].e);
+#pragma unroll
+        for (int t = 0; t < NS; ++t) {
+          const bf16x8 y = values(u.k[kt].c[t], unit);
+#pragma unroll
+          for (int b = 0; b < RB; ++b)
+#pragma unroll
+            for (int i = QP - 1; i >= 0; --i) {
+              const f32x4 acc = t == 0 && i == QP - 1 ? f32x4{0.f, 0.f, 0.f, 0.f} : s[b][kt];
+              s[b][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(y, st.q[b][i][t], acc, 0, 0, 0);
+            }
+        }
+      }
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt) {
+        const float unit = WIDE.value ? unit_down(u.v[kt].e, down) : q4_unit_value(u.v[kt].e);
+        if (!WIDE.value) wide.note(u.v[kt].e);
+#pragma unroll
+        for (int t = 0; t < NS; ++t) *(LDS_AS Vec*)(size_t)(vw[t] + kt * 16 * ROWB) = P::values(u.v[kt].c[t], unit);
+      }
+    };
+    // Then softmax and products.
+    const auto attend = [&]() INLINE {
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      Vec v[DT];
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        const s16x4 y0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4*)(size_t)vr[dt]);
+        const s16x4 y1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4*)(size_t)(vr[dt] + 16 * ROWB));
+        v[dt] = __builtin_bit_cast(Vec, __builtin_shufflevector(y0, y1, 0, 1, 2, 3, 4, 5, 6, 7));
+      }
+      Vec p[RB][PARTS];
+#pragma unroll
+      for (int b = 0; b < RB; ++b) {
+        Exponents t = exponents(s[b], c, st.neg[b]);
+        // lanes exchange their maxima only where some row's moves
+        if (__builtin_amdgcn_ballot_w64(largest(t) > st.above[b]) != 0) {
+          const float m = fmaxf(st.m[b], quad_max(largest(exponents(s[b], 1.f, 0.f)))), mm = m == -INFINITY ? 0.f : m;
+          const float alpha = __builtin_amdgcn_exp2f((st.m[b] - mm) * c);
+          st.l[b] *= alpha;
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt) st.o[b][dt] *= alpha;
+          st.m[b] = m;
+          st.neg[b] = __builtin_fmaf(mm, -c, TOP);
+          st.above[b] = m == -INFINITY ? -INFINITY : TOP + 0.5f;
+          t = exponents(s[b], c, st.neg[b]);
+        }
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; i += 2) {
+          const float y = __builtin_amdgcn_exp2f(t.x[i]), z = __builtin_amdgcn_exp2f(t.x[i + 1]);
+          sum += y;
+          sum += z;
+          P::template split<PARTS>(y, z, p[b], i);
+        }
+        st.l[b] += sum;
+      }
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
         for (int b = 0; b < RB; ++b)
 #pragma unroll
-          for (int i = QP - 1; i >= 0; --i) {
-            const f32x4 acc = t == 0 && i == QP - 1 ? f32x4{0.f, 0.f, 0.f, 0.f} : s[b][kt];
-            s[b][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(y, st.q[b][i][t], acc, 0, 0, 0);
-          }
-      }
+          for (int i = PARTS - 1; i >= 0; --i) st.o[b][dt] = P::multiply(v[dt], p[b][i], st.o[b][dt]);
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+    };
+    int n = 0;
+    for (; n + 1 < n_whole; n += 2) {
+      score(u0);
+      if (n + 2 < n_whole) load_whole(u0, n + 2);
+      attend();
+      score(u1);
+      if (n + 3 < n_whole) load_whole(u1, n + 3);
+      attend();
     }
-#pragma unroll
-    for (int kt = 0; kt < 2; ++kt) {
-      const float unit = q4_unit_value(u.v[kt].e);
-#pragma unroll
-      for (int t = 0; t < NS; ++t) *(LDS_AS bf16x8*)(size_t)(vw[t] + kt * 16 * ROWB) = values(u.v[kt].c[t], unit);
+    if (n < n_whole) {
+      score(u0);
+      attend();
     }
-  };
-  // Then softmax and products.
-  const auto attend = [&] {
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    bf16x8 v[DT];
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt) {
-      const s16x4 y0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4*)(size_t)vr[dt]);
-      const s16x4 y1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4*)(size_t)(vr[dt] + 16 * ROWB));
-      v[dt] = __builtin_shufflevector(__builtin_bit_cast(bf16x4, y0), __builtin_bit_cast(bf16x4, y1), 0, 1, 2, 3, 4, 5, 6, 7);
-    }
-    bf16x8 p[RB][PP];
+    // The units that end past `hi` or among the call's tokens, or that not every row sees.
+    int lim[RB];
 #pragma unroll
     for (int b = 0; b < RB; ++b) {
-      Exponents t = exponents(s[b], c, st.neg[b]);
-      // lanes exchange their maxima only where some row's moves
-      if (__builtin_amdgcn_ballot_w64(largest(t) > st.above[b]) != 0) {
-        const float m = fmaxf(st.m[b], quad_max(largest(exponents(s[b], 1.f, 0.f)))), mm = m == -INFINITY ? 0.f : m;
-        const float alpha = __builtin_amdgcn_exp2f((st.m[b] - mm) * c);
-        st.l[b] *= alpha;
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt) st.o[b][dt] *= alpha;
-        st.m[b] = m;
-        st.neg[b] = mm * -c;
-        st.above[b] = m == -INFINITY ? -INFINITY : 0.f;
-        t = exponents(s[b], c, st.neg[b]);
-      }
-      float sum = 0.f;
-#pragma unroll
-      for (int i = 0; i < 8; i += 2) {
-        const float y = __builtin_amdgcn_exp2f(t.x[i]), z = __builtin_amdgcn_exp2f(t.x[i + 1]);
-        sum += y;
-        sum += z;
-        split_pair<PP>(y, z, p[b], i);
-      }
-      st.l[b] += sum;
+      const int end = a.causal ? cache_len + j[b] + 1 : total;
+      lim[b] = !live[b] ? 0 : end < hi ? end : hi;
     }
+    for (n = n_whole; n < n_units; ++n) {
+      const int key0 = base + n * stride;
+      UnitRegs<D> u;
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt)
+      for (int kt = 0; kt < 2; ++kt) {
+        int key = key0 + 16 * kt + qc;
+        const bool there = key < hi;                 // keys past the last are that one again, masked below
+        key = there ? key : hi - 1;
+        if (key < cached) {
+          load_rows<D, false>(u.k[kt], kc + (size_t)key * (D / 2) + j4 * (D / 8), ks + (size_t)key * (D / 32) + group);
+          load_rows<D, false>(u.v[kt], vc + (size_t)key * (D / 2) + j4 * (D / 8), vs + (size_t)key * (D / 32) + group);
+        }
+        if (__builtin_amdgcn_ballot_w64(key >= cached) != 0) {
+          // (all lanes, so that the lanes of a group meet; those of cached keys keep what they have)
+          const size_t from = (((size_t)beta * a.q_len + (key < cached ? 0 : key - cached)) * g.Hkv + kvh) * D + j4 * (D / 4);
+          const T* src[2] = {(const T*)a.Kn + from, (const T*)a.Vn + from};
+          Rows16<D>* to[2] = {&u.k[kt], &u.v[kt]};
+          unsigned char* codes[2] = {(unsigned char*)a.q4.k_codes, (unsigned char*)a.q4.v_codes};
+          unsigned char* scales[2] = {(unsigned char*)a.q4.k_scales, (unsigned char*)a.q4.v_scales};
 #pragma unroll
-      for (int b = 0; b < RB; ++b)
+          for (int i = 0; i < 2; ++i) {
+            float y[NS][8];
+            uint32_t most = 0;
 #pragma unroll
-        for (int i = PP - 1; i >= 0; --i) st.o[b][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[dt], p[b][i], st.o[b][dt], 0, 0, 0);
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-  };
-  int n = 0;
-  for (; n + 1 < n_whole; n += 2) {
-    score(u0);
-    if (n + 2 < n_whole) load_whole(u0, n + 2);
-    attend();
-    score(u1);
-    if (n + 3 < n_whole) load_whole(u1, n + 3);
-    attend();
-  }
-  if (n < n_whole) {
-    score(u0);
-    attend();
-  }
-  // The units that end past `hi` or among the call's tokens, or that not every row sees.
-  int lim[RB];
+            for (int t = 0; t < NS; ++t) {
+              load8(src[i] + 8 * t, y[t]);
 #pragma unroll
-  for (int b = 0; b < RB; ++b) {
-    const int end = a.causal ? cache_len + j[b] + 1 : total;
-    lim[b] = !live[b] ? 0 : end < hi ? end : hi;
-  }
-  for (n = n_whole; n < n_units; ++n) {
-    const int key0 = base + n * stride;
-    UnitRegs<D> u;
+              for (int e = 0; e < 8; ++e) most = magnitude_bits(y[t][e]) > most ? magnitude_bits(y[t][e]) : most;
+            }
+            if (D == 64) {
+              const uint32_t other = (uint32_t)__shfl_xor((int)most, 16);
+              most = other > most ? other : most;
+            }
+            Rows16<D> r;
+            r.e = q4_unit(most);
 #pragma unroll
-    for (int kt = 0; kt < 2; ++kt) {
-      int key = key0 + 16 * kt + qc;
-      const bool there = key < hi;                 // keys past the last are that one again, masked below
-      key = there ? key : hi - 1;
-      if (key < cached) {
-        load_rows<D, false>(u.k[kt], kc + (size_t)key * (D / 2) + j4 * (D / 8), ks + (size_t)key * (D / 32) + group);
-        load_rows<D, false>(u.v[kt], vc + (size_t)key * (D / 2) + j4 * (D / 8), vs + (size_t)key * (D / 32) + group);
-      }
-      if (__builtin_amdgcn_ballot_w64(key >= cached) != 0) {
-        // (all lanes, so that the lanes of a group meet; those of cached keys keep what they have)
-        const size_t from = (((size_t)beta * a.q_len + (key < cached ? 0 : key - cached)) * g.Hkv + kvh) * D + j4 * (D / 4);
-        const T* src[2] = {(const T*)a.Kn + from, (const T*)a.Vn + from};
-        Rows16<D>* to[2] = {&u.k[kt], &u.v[kt]};
-        unsigned char* codes[2] = {(unsigned char*)a.q4.k_codes, (unsigned char*)a.q4.v_codes};
-        unsigned char* scales[2] = {(unsigned char*)a.q4.k_scales, (unsigned char*)a.q4.v_scales};
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          float y[NS][8];
-          uint32_t most = 0;
-#pragma unroll
-          for (int t = 0; t < NS; ++t) {
-            load8(src[i] + 8 * t, y[t]);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) most = magnitude_bits(y[t][e]) > most ? magnitude_bits(y[t][e]) : most;
-          }
-          if (D == 64) {
-            const uint32_t other = (uint32_t)__shfl_xor((int)most, 16);
-            most = other > most ? other : most;
-          }
-          Rows16<D> r;
-          r.e = q4_unit(most);
-#pragma unroll
-          for (int t = 0; t < NS; ++t) r.c[t] = r.e == 255u ? 0u : q4_codes(y[t], q4_unit_value(r.e));
-          if (key < cached) continue;
-          *to[i] = r;
-          if (there && tile == 0) {
-            unsigned char* at = codes[i] + (rows0 + key) * (D / 2) + j4 * (D / 8);
-            if constexpr (D == 128) *(i32x4*)at = i32x4{(int)r.c[0], (int)r.c[1], (int)r.c[2], (int)r.c[3]};
-            else *(i32x2*)at = i32x2{(int)r.c[0], (int)r.c[1]};
-            if (D == 128 || (j4 & 1) == 0) scales[i][(rows0 + key) * (D / 32) + group] = (unsigned char)r.e;
+            for (int t = 0; t < NS; ++t) r.c[t] = r.e == 255u ? 0u : q4_codes(y[t], q4_unit_value(r.e));
+            if (key < cached) continue;
+            *to[i] = r;
+            if (there && tile == 0) {
+              unsigned char* at = codes[i] + (rows0 + key) * (D / 2) + j4 * (D / 8);
+              if constexpr (D == 128) *(i32x4*)at = i32x4{(int)r.c[0], (int)r.c[1], (int)r.c[2], (int)r.c[3]};
+              else *(i32x2*)at = i32x2{(int)r.c[0], (int)r.c[1]};
+              if (D == 128 || (j4 & 1) == 0) scales[i][(rows0 + key) * (D / 32) + group] = (unsigned char)r.e;
+            }
           }
         }
       }
-    }
-    // A value that is NaN counts where its key is seen and nowhere else, and its weight may be zero where it is not: it goes
-    // to the outputs of the rows that see it, and zeros to the products.
-    uint64_t bad[2];
+      // A value that is NaN counts where its key is seen and nowhere else, and its weight may be zero where it is not: it goes
+      // to the outputs of the rows that see it, and zeros to the products.
+      uint64_t bad[2];
 #pragma unroll
-    for (int kt = 0; kt < 2; ++kt) {
-      bad[kt] = __builtin_amdgcn_ballot_w64(u.v[kt].e == 255u);
-      if (u.v[kt].e == 255u) {
-        u.v[kt].e = 127;
+      for (int kt = 0; kt < 2; ++kt) {
+        bad[kt] = __builtin_amdgcn_ballot_w64(u.v[kt].e == 255u);
+        if (u.v[kt].e == 255u) {
+          u.v[kt].e = 127;
 #pragma unroll
-        for (int t = 0; t < NS; ++t) u.v[kt].c[t] = 0;
+          for (int t = 0; t < NS; ++t) u.v[kt].c[t] = 0;
+        }
       }
-    }
-    score(u);
+      score(u);
 #pragma unroll
-    for (int b = 0; b < RB; ++b) {
-      const int room = lim[b] - key0 - 4 * j4;      // element (kt, e) is key key0 + 16 kt + 4 j4 + e
+      for (int b = 0; b < RB; ++b) {
+        const int room = lim[b] - key0 - 4 * j4;      // element (kt, e) is key key0 + 16 kt + 4 j4 + e
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[b][kt][e] = 16 * kt + e < room ? s[b][kt][e] : -INFINITY;
+      }
+      attend();
 #pragma unroll
       for (int kt = 0; kt < 2; ++kt)
+        for (uint64_t left = bad[kt]; left; left &= left - 1) {
+          const int at = __builtin_ctzll(left), key = key0 + 16 * kt + (at & 15);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s[b][kt][e] = 16 * kt + e < room ? s[b][kt][e] : -INFINITY;
+          for (int b = 0; b < RB; ++b)
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt)                  // lane at / 16 had columns D / 4 (at / 16) ..
+              if (key < lim[b] && dt / (DT / 4) == at >> 4) st.o[b][dt] = f32x4{NAN, NAN, NAN, NAN};
+        }
     }
-    attend();
+
+  };
+  walk(std::integral_constant<bool, false>());
+  __shared__ int lds_wide[WAVES];
+  if (lane == 0) lds_wide[wave] = wide.flags();
+  __syncthreads();
+  int any_wide = 0;
 #pragma unroll
-    for (int kt = 0; kt < 2; ++kt)
-      for (uint64_t left = bad[kt]; left; left &= left - 1) {
-        const int at = __builtin_ctzll(left), key = key0 + 16 * kt + (at & 15);
-#pragma unroll
-        for (int b = 0; b < RB; ++b)
-#pragma unroll
-          for (int dt = 0; dt < DT; ++dt)                  // lane at / 16 had columns D / 4 (at / 16) ..
-            if (key < lim[b] && dt / (DT / 4) == at >> 4) st.o[b][dt] = f32x4{NAN, NAN, NAN, NAN};
-      }
+  for (int k = 0; k < WAVES; ++k) any_wide |= lds_wide[k];
+  if (__builtin_expect(__builtin_amdgcn_readfirstlane(any_wide) != 0, 0)) {
+    down = any_wide & 2 ? DOWN : 0;
+    walk(std::integral_constant<bool, true>());
   }
 
+  const float up = down ? __builtin_ldexpf(1.f, DOWN) : 1.f;
   // the wavefronts meet, in a fixed order
 #pragma unroll
   for (int b = 0; b < RB; ++b) {
@@ -434,11 +460,11 @@ __global__ __launch_bounds__(64 * WAVES, 2) void q4_stream_kernel(Q4Args a, Stre
     for (int k = 0; k < WAVES; ++k) lt += lds_l[k][16 * b + qc] * __builtin_amdgcn_exp2f((lds_m[k][16 * b + qc] - mm) * c);
     const float scale = lt == 0.f ? 0.f : __builtin_amdgcn_exp2f((st.m[b] - mm) * c) * (1.f / lt);
     if (threadIdx.x < 16 && live[b])
-      a.LSE_sub[out0 + (size_t)head[b] * a.q_len + j[b]] = lt == 0.f ? -INFINITY : (mm * c + __builtin_amdgcn_logf(lt)) * LN2;
+      a.LSE_sub[out0 + (size_t)head[b] * a.q_len + j[b]] = lt == 0.f ? -INFINITY : (mm * c - TOP + __builtin_amdgcn_logf(lt)) * LN2;
     float* mine = meet + wave * 16 * D + qc * D;
     if (b > 0) __syncthreads();
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt) *(f32x4*)(mine + ((4 * dt + j4) ^ qc) * 4) = st.o[b][dt] * scale;
+    for (int dt = 0; dt < DT; ++dt) *(f32x4*)(mine + ((4 * dt + j4) ^ qc) * 4) = st.o[b][dt] * scale * up;
     __syncthreads();
     for (int i = threadIdx.x; i < 16 * (D / 4); i += 64 * WAVES) {
       const int r = i / (D / 4), chunk = i % (D / 4), row = tile * 16 * RB + 16 * b + r;
@@ -478,7 +504,7 @@ hipError_t launch_phase2_q4_stream(int dtype, const Q4Args& a, hipStream_t st) {
   if (rows > a.plan.tile_rows || a.plan.tile_rows != (rows <= 16 ? 16 : 32)) return hipErrorInvalidValue;
   if (dtype == 0) {
     if (rows > 16) return hipErrorInvalidValue;
-    return a.g.d == 64 ? launch_stream<float, 64, 3, 1>(a, st) : launch_stream<float, 128, 3, 1>(a, st);
+    return a.g.d == 64 ? launch_stream<float, 64, 2, 1>(a, st) : launch_stream<float, 128, 2, 1>(a, st);
   }
   if (rows <= 16) return a.parts == 2 ? launch_stream<__bf16, 128, 2, 1>(a, st) : launch_stream<__bf16, 128, 1, 1>(a, st);
   return a.parts == 2 ? launch_stream<__bf16, 128, 2, 2>(a, st) : launch_stream<__bf16, 128, 1, 2>(a, st);

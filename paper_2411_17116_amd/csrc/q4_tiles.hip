@@ -5,7 +5,7 @@
 //     while the ones before are read, a barrier per tile.  Codes are requested a tile ahead of that.
 //   * S^T = K Q^T, the exponentiated scores are the B operand of O^T += V^T P^T, as in the stream (q4.hip).  A stage of 32 keys has the scores of unit
 //     u + 1, the exponentials of unit u and the products of unit u - 1, which do not wait for each other.
-//   * The reference of a row's exponentials is a whole power of two that moves where a weight would pass 2^8: what has been summed up so far, and the weights
+//   * The reference of a row's exponentials is a whole power of two that moves where a weight would pass 2^15: what has been summed up so far, and the weights
 //     of the unit on its way, are then multiplied by a power of two, which loses nothing, in a branch of its own.
 #include "q4_attend.h"
 
@@ -19,7 +19,7 @@ typedef const __attribute__((address_space(1))) unsigned char* GlobalBytes;
 
 constexpr int KEYS = 64;              // of a tile
 constexpr int THREADS = 512;
-constexpr float HEADROOM = 8.f;       // powers of two a weight may pass one by
+constexpr float HEADROOM = 4.f;       // a reference is set where the largest weight is 2^(TOP - 3) or down to half that, and moves where one passes 2^(TOP + 1)
 
 struct TileDiv {
   Div Hkv, tiles, splits, G;
@@ -32,7 +32,7 @@ struct Raw {                          // a thread's codes of a tile: E elements 
   uint32_t e;
 };
 
-template <int QP, int PP, int NS, int DT, int RB>
+template <int QP, int NS, int DT, int RB>
 struct Rows {
   bf16x8 q[RB][QP][NS];
   f32x4 o[RB][DT];
@@ -71,9 +71,9 @@ __global__ __launch_bounds__(THREADS, 2) void q4_tiles_kernel(Q4Args a, TileDiv 
   const int lo = (int)lo64, hi = (int)hi64;
   const int all_tiles = hi > lo ? (hi - lo + KEYS - 1) / KEYS : 0;
   const int n_tiles = H == 1 ? all_tiles : (all_tiles - ring + 1) / 2, most_tiles = H == 1 ? all_tiles : (all_tiles + 1) / 2;
-  const auto key_of = [&](int t) { return lo + KEYS * (H == 1 ? t : 2 * t + ring); };
+  const auto key_of = [&](int t) INLINE { return lo + KEYS * (H == 1 ? t : 2 * t + ring); };
 
-  Rows<QP, PP, NS, DT, RB> r;
+  Rows<QP, NS, DT, RB> r;
   int lim[RB];
 #pragma unroll
   for (int b = 0; b < RB; ++b) {
@@ -90,19 +90,14 @@ __global__ __launch_bounds__(THREADS, 2) void q4_tiles_kernel(Q4Args a, TileDiv 
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         __bf16 part[QP];
-        split<QP>(live ? y[e] : 0.f, part);
+        split(live ? y[e] : 0.f, part);
 #pragma unroll
         for (int i = 0; i < QP; ++i) r.q[b][i][t][e] = part[i];
       }
     }
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt) r.o[b][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
-    r.ref[b] = 0.f;
-    r.above[b] = -INFINITY;
-    r.l[b] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
   // Keys from which on some row does not see all: of the workgroup, and of the wavefront
-  const auto seen_by_all = [&](int row) {
+  const auto seen_by_all = [&](int row) INLINE {
     const int end = a.causal && row < R ? cache_len + (int)quotient(row, by.G) + 1 : total;
     return end < hi ? end : hi;
   };
@@ -116,7 +111,7 @@ __global__ __launch_bounds__(THREADS, 2) void q4_tiles_kernel(Q4Args a, TileDiv 
   const int my_key = tid / PER, my_col = tid % PER * E;
   const unsigned c_off = my_key * (D / 2) + my_col / 2, s_off = my_key * (D / 32) + my_col / 32;
   const int whole_hi = hi < cached ? hi : cached;
-  const auto take = [&](RawT& raw, GlobalBytes codes, GlobalBytes scales) {
+  const auto take = [&](RawT& raw, GlobalBytes codes, GlobalBytes scales) INLINE {
     if constexpr (E == 32) {
       const i32x4 y = *(const __attribute__((address_space(1))) i32x4*)codes;
 #pragma unroll
@@ -130,7 +125,7 @@ __global__ __launch_bounds__(THREADS, 2) void q4_tiles_kernel(Q4Args a, TileDiv 
     }
     raw.e = *scales;
   };
-  const auto request = [&](RawT& raw, bool v, int t) {
+  const auto request = [&](RawT& raw, bool v, int t) INLINE {
     const unsigned char* codes = (const unsigned char*)(v ? a.q4.v_codes : a.q4.k_codes);
     const unsigned char* scales = (const unsigned char*)(v ? a.q4.v_scales : a.q4.k_scales);
     if (__builtin_expect(key_of(t) + KEYS <= whole_hi, 1)) {
@@ -178,32 +173,15 @@ __global__ __launch_bounds__(THREADS, 2) void q4_tiles_kernel(Q4Args a, TileDiv 
 #pragma unroll
   for (int i = 0; i < E / 8; ++i) put[i] = lds0 + my_key * ROWB + (((my_col / 8 + (E == 16 ? i ^ (my_key & 1) : i)) ^ swz<D>(my_key & 15)) << 4);
   const uint32_t swapped = E == 16 && (my_key & 1) ? 0xffffffffu : 0u;
-  const auto file = [&](const RawT& raw, unsigned buffer) {
-    const float unit = q4_unit_value(raw.e);
+  const auto file = [&](auto AS, const RawT& raw, unsigned buffer, int below = 0) INLINE {
+    const float unit = below ? unit_down(raw.e, below) : q4_unit_value(raw.e);
 #pragma unroll
     for (int i = 0; i < E / 8; ++i) {
       // (two chunks a thread: the first of every second key's threads is the odd one, so that they spread over all slots)
       const uint32_t code = E == 16 ? (swapped & raw.c[(i ^ 1) % (E / 8)]) | (~swapped & raw.c[i]) : raw.c[i];
-      *(LDS_AS bf16x8*)(size_t)(put[i] + buffer) = values(code, unit);
+      *(LDS_AS typename decltype(AS)::Vec*)(size_t)(put[i] + buffer) = decltype(AS)::values(code, unit);
     }
   };
-  // V of a tile that not every row sees: its NaN go to the rows that see them, behind the products (see below).
-  const auto file_v = [&](RawT& raw, int t, unsigned buffer) {
-    if (key_of(t) + KEYS > wg_free) {
-      if (my_col % 32 == 0) {
-        unsigned char* at = (unsigned char*)&lds_e[ring][t & 1][my_key];
-        at[my_col / 32] = (unsigned char)raw.e;
-        if (D == 64 && my_col == 0) at[2] = at[3] = 0;
-      }
-      if (raw.e == 255u) {
-        raw.e = 127;
-#pragma unroll
-        for (int i = 0; i < E / 8; ++i) raw.c[i] = 0;
-      }
-    }
-    file(raw, buffer);
-  };
-
   // ---- operands from LDS
   unsigned ka[NS], va[DT];
 #pragma unroll
@@ -212,255 +190,303 @@ __global__ __launch_bounds__(THREADS, 2) void q4_tiles_kernel(Q4Args a, TileDiv 
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt) va[dt] = lds0 + 2 * TILEB + rr * ROWB + (((2 * dt + ((lane & 3) >> 1)) ^ swz<D>(rr)) << 4) + 8 * (lane & 1);
 
-  typedef Scores<RB> S;
-  typedef bf16x8 Weights[RB][PP];
-  static_assert(2 * NS == DT, "as many operands of K as of V in 32 keys");
-  // K operand f of a unit: keys 16 (f % 2) .. +15, step f / 2 of the products.  V operand f: columns 16 f .. +15; slot e is key 4 j4 + e or 16 + 4 j4 + e - 4, as in
-  // the weights.
-  const auto read_k = [&](int f, unsigned at) { return *(LDS_AS bf16x8*)(size_t)(ka[f >> 1] + at + (f & 1) * 16 * ROWB); };
-  const auto read_v = [&](int f, unsigned at) {
-    const s16x4 y0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4*)(size_t)(va[f] + at));
-    const s16x4 y1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4*)(size_t)(va[f] + at + 16 * ROWB));
-    return __builtin_shufflevector(__builtin_bit_cast(bf16x4, y0), __builtin_bit_cast(bf16x4, y1), 0, 1, 2, 3, 4, 5, 6, 7);
-  };
-  const auto score_by = [&](S& s, const bf16x8& y, int f) {
+  Wide wide = {0, 0};
+  int down = 0;
+  const auto walk = [&](auto WIDE) INLINE {
+    typedef Product<WIDE.value> P;
+    typedef typename P::Vec Vec;
+    typedef std::remove_reference_t<decltype(Vec()[0])> Elem;
+    constexpr int PARTS = WIDE.value && PP > 1 ? 3 : PP;
 #pragma unroll
-    for (int b = 0; b < RB; ++b)
+    for (int b = 0; b < RB; ++b) {
 #pragma unroll
-      for (int i = QP - 1; i >= 0; --i) {
-        const f32x4 acc = f < 2 && i == QP - 1 ? f32x4{0.f, 0.f, 0.f, 0.f} : s.s[b][f & 1];
-        s.s[b][f & 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(y, r.q[b][i][f >> 1], acc, 0, 0, 0);
+      for (int dt = 0; dt < DT; ++dt) r.o[b][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+      r.ref[b] = 0.f;
+      r.above[b] = -INFINITY;
+      r.l[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    // V of a tile that not every row sees: its NaN go to the rows that see them, behind the products (see below).
+    const auto file_v = [&](RawT& raw, int t, unsigned buffer) INLINE {
+      if (key_of(t) + KEYS > wg_free) {
+        if (my_col % 32 == 0) {
+          unsigned char* at = (unsigned char*)&lds_e[ring][t & 1][my_key];
+          at[my_col / 32] = (unsigned char)raw.e;
+          if (D == 64 && my_col == 0) at[2] = at[3] = 0;
+        }
+        if (raw.e == 255u) {
+          raw.e = 127;
+#pragma unroll
+          for (int i = 0; i < E / 8; ++i) raw.c[i] = 0;
+        }
       }
-  };
-  const auto multiply_by = [&](const Weights& p, const bf16x8& y, int f) {
-#pragma unroll
-    for (int n = 0; n < RB; ++n) {
-      const int b = f & 1 ? RB - 1 - n : n;       // (the same operand twice in a row where rows change)
-#pragma unroll
-      for (int i = PP - 1; i >= 0; --i) r.o[b][f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(y, p[b][i], r.o[b][f], 0, 0, 0);
-    }
-  };
-  const auto mask = [&](S& s, int key0) {
-    asm volatile("");                             // (a branch of its own: few tiles want it)
-#pragma unroll
-    for (int b = 0; b < RB; ++b) {
-      const int room = lim[b] - key0 - 4 * j4;      // element (kt, e) is key key0 + 16 kt + 4 j4 + e
-#pragma unroll
-      for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) s.s[b][kt][e] = 16 * kt + e < room ? s.s[b][kt][e] : -INFINITY;
-    }
-  };
-  // Exponents of a unit's weights; the references of its rows are raised first, where it asks for it.  `p`: weights against the ones before.
-  typedef Exponents Powers[RB];
-  const auto raise = [&](const S& s, Powers& x, Weights& p) {
-    bool far = false;
-#pragma unroll
-    for (int b = 0; b < RB; ++b) {
-      x[b] = exponents(s.s[b], c, -r.ref[b]);
-      far |= largest(x[b]) > r.above[b];
-    }
-    if (__builtin_expect(__builtin_amdgcn_ballot_w64(far) == 0, 1)) return;
-#pragma unroll
-    for (int b = 0; b < RB; ++b) {
-      const float top = __builtin_ceilf(quad_max(largest(exponents(s.s[b], c, 0.f))));
-      const bool none = r.above[b] == -INFINITY;                       // nothing was seen
-      const float ref = none ? (top == -INFINITY ? 0.f : top) : fmaxf(r.ref[b], top);
-      const float alpha = none ? 0.f : __builtin_amdgcn_exp2f(r.ref[b] - ref);
-      r.ref[b] = ref;
-      r.above[b] = none && top == -INFINITY ? -INFINITY : HEADROOM;
-      r.l[b] *= alpha;
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt) r.o[b][dt] *= alpha;
-#pragma unroll
-      for (int i = 0; i < PP; ++i)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) p[b][i][e] = (__bf16)((float)p[b][i][e] * alpha);
-      x[b] = exponents(s.s[b], c, -ref);
-    }
-  };
-  const auto weigh = [&](const Powers& x, Weights& p) {
-#pragma unroll
-    for (int b = 0; b < RB; ++b)
-#pragma unroll
-      for (int i = 0; i < 8; i += 2) split_pair<PP>(__builtin_amdgcn_exp2f(x[b].x[i]), __builtin_amdgcn_exp2f(x[b].x[i + 1]), p[b], i);
-  };
-  // The sums of the weights, as they are multiplied: products with ones in row 0, whose element 0 is the lanes' with j4 = 0.
-  const __bf16 one = qc == 0 ? (__bf16)1.f : (__bf16)0.f;
-  const bf16x8 ones = {one, one, one, one, one, one, one, one};
-  const auto sum_up = [&](const Weights& p) {
-#pragma unroll
-    for (int b = 0; b < RB; ++b)
-#pragma unroll
-      for (int i = PP - 1; i >= 0; --i) r.l[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, p[b][i], r.l[b], 0, 0, 0);
-  };
+      wide.note(raw.e);
+      file(P(), raw, buffer, WIDE.value ? down : 0);
+    };
 
-  RawT rk, rv;
-  // A stage: scores of a unit (K at `k`), weights of the one before, products of the one before that (V at `v`).  The order of instructions is pinned:
-  // a few of the vector unit's between two products, operands read ahead.
-  // FILE: codes are put into LDS on the way (K at `to_k`, V at `to_v`).
-  constexpr std::integral_constant<bool, true> FILED;
-  constexpr std::integral_constant<bool, false> NOT_FILED;
-  const auto stage = [&](auto FILE, S& next, unsigned k, Powers& now, Weights& p, const Weights& before, unsigned v, unsigned to_k, unsigned to_v) {
-#pragma unroll
-    for (int b = 0; b < RB; ++b)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) asm volatile("" : "+v"(now[b].x[i]));      // (weights stay in their stage)
-    bf16x8 kf[DT], vf[DT];
-#pragma unroll
-    for (int f = 0; f < DT; ++f) { kf[f] = read_k(f, k); vf[f] = read_v(f, v); }
-    weigh(now, p);
-    if constexpr (FILE.value) {
-      file(rk, to_k);
-      file(rv, to_v);
-    }
-#pragma unroll
-    for (int f = 0; f < DT; f += 2) {
-      score_by(next, kf[f], f);
-      score_by(next, kf[f + 1], f + 1);
-      multiply_by(before, vf[f], f);
-      multiply_by(before, vf[f + 1], f + 1);
-    }
-    sum_up(before);
-    constexpr int PRODUCTS = RB * (DT * (QP + PP) + PP), OPS = RB * (PP == 1 ? 12 : PP == 2 ? 32 : 52) + (FILE.value ? E + 8 : 0), READS = 3 * DT;
-    constexpr int PER = (OPS + PRODUCTS - 1) / PRODUCTS, EVERY = RB * (QP + PP);
-    __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
-#pragma unroll
-    for (int i = 0; i < PRODUCTS; ++i) {
-      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-      if (i % EVERY == EVERY - 1 && 6 + i / EVERY * 3 < READS) __builtin_amdgcn_sched_group_barrier(0x100, 3, 0);
-      __builtin_amdgcn_sched_group_barrier(0x002, PER, 0);
-      if (FILE.value && i % EVERY == EVERY - 1 && i / EVERY >= DT - E / 4 && i / EVERY < DT) __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);
-    }
-#pragma unroll
-    for (int b = 0; b < RB; ++b) {
-#pragma unroll
-      for (int i = 0; i < PP; ++i) asm volatile("" : "+v"(p[b][i]));
-    }
-    __builtin_amdgcn_sched_barrier(0);
-  };
-  const auto score = [&](S& s, unsigned k) {
-#pragma unroll
-    for (int f = 0; f < DT; ++f) score_by(s, read_k(f, k), f);
-  };
-  const auto multiply = [&](const Weights& p, unsigned v) {
-#pragma unroll
-    for (int f = 0; f < DT; ++f) multiply_by(p, read_v(f, v), f);
-    sum_up(p);
-  };
-
-  const auto barrier = [] {
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
-    __builtin_amdgcn_s_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");
-  };
-  S sA, sB;
-  Weights pA, pB;
-  Powers x;
-  if (n_tiles > 0) {
-    request(rk, false, 0);
-    request(rv, true, 0);
-    file(rk, 0);
-    file_v(rv, 0, 2 * TILEB);
-    if (n_tiles > 1) {
-      request(rk, false, 1);
-      request(rv, true, 1);
-      file(rk, TILEB);
-      if (n_tiles > 2) request(rk, false, 2);
-    }
-  }
-#pragma unroll
-  for (int b = 0; b < RB; ++b)
-#pragma unroll
-    for (int i = 0; i < PP; ++i) pA[b][i] = bf16x8{0, 0, 0, 0, 0, 0, 0, 0};
-  barrier();
-  if (n_tiles > 0) {
-    score(sA, 0);
-    score(sB, UNITB);
-    const int key0 = key_of(0);
-    if (key0 + KEYS > wave_free) { mask(sA, key0); mask(sB, key0 + 32); }
-    raise(sA, x, pA);
-    weigh(x, pA);
-  }
-  // A value that is NaN counts where its key is seen and nowhere else, and its weight may be zero where it is not.
-  const auto not_numbers = [&](int t) {
-    const int key0 = key_of(t);
-    if (key0 + KEYS <= wg_free) return;
-    const uint32_t e = lds_e[ring][t & 1][lane];
-    bool nan = false;
-#pragma unroll
-    for (int k = 0; k < D / 32; ++k) nan |= (e >> (8 * k) & 255u) == 255u;
-    for (uint64_t left = __builtin_amdgcn_ballot_w64(nan); left; left &= left - 1) {
-      const int key = __builtin_ctzll(left);
-      const uint32_t which = lds_e[ring][t & 1][key];
+    typedef Scores<RB> S;
+    typedef Vec Weights[RB][PARTS];
+    static_assert(2 * NS == DT, "as many operands of K as of V in 32 keys");
+    // K operand f of a unit: keys 16 (f % 2) .. +15, step f / 2 of the products.  V operand f: columns 16 f .. +15; slot e is key 4 j4 + e or 16 + 4 j4 + e - 4, as in
+    // the weights.
+    const auto read_k = [&](int f, unsigned at) INLINE { return *(LDS_AS bf16x8*)(size_t)(ka[f >> 1] + at + (f & 1) * 16 * ROWB); };
+    const auto read_v = [&](int f, unsigned at) INLINE {
+      const s16x4 y0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4*)(size_t)(va[f] + at));
+      const s16x4 y1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4*)(size_t)(va[f] + at + 16 * ROWB));
+      return __builtin_bit_cast(Vec, __builtin_shufflevector(y0, y1, 0, 1, 2, 3, 4, 5, 6, 7));
+    };
+    const auto score_by = [&](S& s, const bf16x8& y, int f) INLINE {
 #pragma unroll
       for (int b = 0; b < RB; ++b)
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt)
-          if (key0 + key < lim[b] && (which >> (8 * (dt / 2)) & 255u) == 255u) r.o[b][dt] = f32x4{NAN, NAN, NAN, NAN};
+        for (int i = QP - 1; i >= 0; --i) {
+          const f32x4 acc = f < 2 && i == QP - 1 ? f32x4{0.f, 0.f, 0.f, 0.f} : s.s[b][f & 1];
+          s.s[b][f & 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(y, r.q[b][i][f >> 1], acc, 0, 0, 0);
+        }
+    };
+    const auto multiply_by = [&](const Weights& p, const Vec& y, int f) INLINE {
+#pragma unroll
+      for (int n = 0; n < RB; ++n) {
+        const int b = f & 1 ? RB - 1 - n : n;       // (the same operand twice in a row where rows change)
+#pragma unroll
+        for (int i = PARTS - 1; i >= 0; --i) r.o[b][f] = P::multiply(y, p[b][i], r.o[b][f]);
+      }
+    };
+    const auto mask = [&](S& s, int key0) INLINE {
+      asm volatile("");                             // (a branch of its own: few tiles want it)
+#pragma unroll
+      for (int b = 0; b < RB; ++b) {
+        const int room = lim[b] - key0 - 4 * j4;      // element (kt, e) is key key0 + 16 kt + 4 j4 + e
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s.s[b][kt][e] = 16 * kt + e < room ? s.s[b][kt][e] : -INFINITY;
+      }
+    };
+    // Exponents of a unit's weights; the references of its rows are raised first, where it asks for it.  `p`: weights against the ones before.
+    typedef Exponents Powers[RB];
+    const auto raise = [&](const S& s, Powers& x, Weights& p) INLINE {
+      bool far = false;
+#pragma unroll
+      for (int b = 0; b < RB; ++b) {
+        x[b] = exponents(s.s[b], c, -r.ref[b]);
+        far |= largest(x[b]) > r.above[b];
+      }
+      if (__builtin_expect(__builtin_amdgcn_ballot_w64(far) == 0, 1)) return;
+#pragma unroll
+      for (int b = 0; b < RB; ++b) {
+        const float top = __builtin_ceilf(quad_max(largest(exponents(s.s[b], c, 0.f)))) - (TOP + 1 - HEADROOM);
+        const bool none = r.above[b] == -INFINITY;                       // nothing was seen
+        const float ref = none ? (top == -INFINITY ? 0.f : top) : fmaxf(r.ref[b], top);
+        const float alpha = none ? 0.f : __builtin_amdgcn_exp2f(r.ref[b] - ref);
+        r.ref[b] = ref;
+        r.above[b] = none && top == -INFINITY ? -INFINITY : TOP + 1;
+        r.l[b] *= alpha;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) r.o[b][dt] *= alpha;
+#pragma unroll
+        for (int i = 0; i < PARTS; ++i)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) p[b][i][e] = (Elem)((float)p[b][i][e] * alpha);
+        x[b] = exponents(s.s[b], c, -ref);
+      }
+    };
+    const auto weigh = [&](const Powers& x, Weights& p) INLINE {
+#pragma unroll
+      for (int b = 0; b < RB; ++b)
+#pragma unroll
+        for (int i = 0; i < 8; i += 2) P::template split<PARTS>(__builtin_amdgcn_exp2f(x[b].x[i]), __builtin_amdgcn_exp2f(x[b].x[i + 1]), p[b], i);
+    };
+    // The sums of the weights, as they are multiplied: products with ones in row 0, whose element 0 is the lanes' with j4 = 0.
+    const Elem one = qc == 0 ? (Elem)1.f : (Elem)0.f;
+    const Vec ones = {one, one, one, one, one, one, one, one};
+    const auto sum_up = [&](const Weights& p) INLINE {
+#pragma unroll
+      for (int b = 0; b < RB; ++b)
+#pragma unroll
+        for (int i = PARTS - 1; i >= 0; --i) r.l[b] = P::multiply(ones, p[b][i], r.l[b]);
+    };
+
+    RawT rk, rv;
+    // A stage: scores of a unit (K at `k`), weights of the one before, products of the one before that (V at `v`).  The order of instructions is pinned:
+    // a few of the vector unit's between two products, operands read ahead.
+    // FILE: codes are put into LDS on the way (K at `to_k`, V at `to_v`).
+    constexpr std::integral_constant<bool, true> FILED;
+    constexpr std::integral_constant<bool, false> NOT_FILED;
+    const auto stage = [&](auto FILE, S& next, unsigned k, Powers& now, Weights& p, const Weights& before, unsigned v, unsigned to_k, unsigned to_v) INLINE {
+#pragma unroll
+      for (int b = 0; b < RB; ++b)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) asm volatile("" : "+v"(now[b].x[i]));      // (weights stay in their stage)
+      bf16x8 kf[DT];
+      Vec vf[DT];
+#pragma unroll
+      for (int f = 0; f < DT; ++f) { kf[f] = read_k(f, k); vf[f] = read_v(f, v); }
+      weigh(now, p);
+      if constexpr (FILE.value) {
+        file(Product<true>(), rk, to_k);
+        wide.note(rv.e);
+        file(P(), rv, to_v, WIDE.value ? down : 0);
+      }
+#pragma unroll
+      for (int f = 0; f < DT; f += 2) {
+        score_by(next, kf[f], f);
+        score_by(next, kf[f + 1], f + 1);
+        multiply_by(before, vf[f], f);
+        multiply_by(before, vf[f + 1], f + 1);
+      }
+      sum_up(before);
+      constexpr int PRODUCTS = RB * (DT * (QP + PARTS) + PARTS), OPS = RB * (PARTS == 1 ? 12 : PARTS == 2 ? 24 : 52) + (FILE.value ? E + 8 : 0), READS = 3 * DT;
+      constexpr int PER = (OPS + PRODUCTS - 1) / PRODUCTS, EVERY = RB * (QP + PARTS);
+      __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
+#pragma unroll
+      for (int i = 0; i < PRODUCTS; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        if (i % EVERY == EVERY - 1 && 6 + i / EVERY * 3 < READS) __builtin_amdgcn_sched_group_barrier(0x100, 3, 0);
+        __builtin_amdgcn_sched_group_barrier(0x002, PER, 0);
+        if (FILE.value && i % EVERY == EVERY - 1 && i / EVERY >= DT - E / 4 && i / EVERY < DT) __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);
+      }
+#pragma unroll
+      for (int b = 0; b < RB; ++b) {
+#pragma unroll
+        for (int i = 0; i < PARTS; ++i) asm volatile("" : "+v"(p[b][i]));
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    const auto score = [&](S& s, unsigned k) INLINE {
+#pragma unroll
+      for (int f = 0; f < DT; ++f) score_by(s, read_k(f, k), f);
+    };
+    const auto multiply = [&](const Weights& p, unsigned v) INLINE {
+#pragma unroll
+      for (int f = 0; f < DT; ++f) multiply_by(p, read_v(f, v), f);
+      sum_up(p);
+    };
+
+    const auto barrier = []() INLINE {
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
+      __builtin_amdgcn_s_barrier();
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");
+    };
+    S sA, sB;
+    Weights pA, pB;
+    Powers x;
+    if (n_tiles > 0) {
+      request(rk, false, 0);
+      request(rv, true, 0);
+      file(Product<true>(), rk, 0);
+      file_v(rv, 0, 2 * TILEB);
+      if (n_tiles > 1) {
+        request(rk, false, 1);
+        request(rv, true, 1);
+        file(Product<true>(), rk, TILEB);
+        if (n_tiles > 2) request(rk, false, 2);
+      }
     }
-  };
-  // Tile t: its V is multiplied while K of tile t + 1 makes the next scores, K of tile t + 2 and V of tile t + 1 are filed.
-  const auto step = [&](int t, unsigned odd) {      // odd: TILEB for odd t
-    const unsigned even = TILEB - odd;
+#pragma unroll
+    for (int b = 0; b < RB; ++b)
+#pragma unroll
+      for (int i = 0; i < PARTS; ++i) pA[b][i] = Vec{0, 0, 0, 0, 0, 0, 0, 0};
     barrier();
-    if (t + 2 < n_tiles) file(rk, odd);
-    file_v(rv, t + 1, 2 * TILEB + even);
-    if (t + 3 < n_tiles) request(rk, false, t + 3);
-    if (t + 2 < n_tiles) request(rv, true, t + 2);
-    const int key1 = key_of(t + 1);
-    const bool partly = key1 + KEYS > wave_free;
-    raise(sB, x, pA);
-    stage(NOT_FILED, sA, even, x, pB, pA, odd, 0, 0);
-    if (__builtin_expect(partly, 0)) mask(sA, key1);
-    raise(sA, x, pB);
-    stage(NOT_FILED, sB, even + UNITB, x, pA, pB, odd + UNITB, 0, 0);
-    if (__builtin_expect(partly, 0)) mask(sB, key1 + 32);
-    not_numbers(t);
+    if (n_tiles > 0) {
+      score(sA, 0);
+      score(sB, UNITB);
+      const int key0 = key_of(0);
+      if (key0 + KEYS > wave_free) { mask(sA, key0); mask(sB, key0 + 32); }
+      raise(sA, x, pA);
+      weigh(x, pA);
+    }
+    // A value that is NaN counts where its key is seen and nowhere else, and its weight may be zero where it is not.
+    const auto not_numbers = [&](int t) INLINE {
+      const int key0 = key_of(t);
+      if (key0 + KEYS <= wg_free) return;
+      const uint32_t e = lds_e[ring][t & 1][lane];
+      bool nan = false;
+#pragma unroll
+      for (int k = 0; k < D / 32; ++k) nan |= (e >> (8 * k) & 255u) == 255u;
+      for (uint64_t left = __builtin_amdgcn_ballot_w64(nan); left; left &= left - 1) {
+        const int key = __builtin_ctzll(left);
+        const uint32_t which = lds_e[ring][t & 1][key];
+#pragma unroll
+        for (int b = 0; b < RB; ++b)
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt)
+            if (key0 + key < lim[b] && (which >> (8 * (dt / 2)) & 255u) == 255u) r.o[b][dt] = f32x4{NAN, NAN, NAN, NAN};
+      }
+    };
+    // Tile t: its V is multiplied while K of tile t + 1 makes the next scores, K of tile t + 2 and V of tile t + 1 are filed.
+    const auto step = [&](int t, unsigned odd) INLINE {      // odd: TILEB for odd t
+      const unsigned even = TILEB - odd;
+      barrier();
+      if (t + 2 < n_tiles) file(Product<true>(), rk, odd);
+      file_v(rv, t + 1, 2 * TILEB + even);
+      if (t + 3 < n_tiles) request(rk, false, t + 3);
+      if (t + 2 < n_tiles) request(rv, true, t + 2);
+      const int key1 = key_of(t + 1);
+      const bool partly = key1 + KEYS > wave_free;
+      raise(sB, x, pA);
+      stage(NOT_FILED, sA, even, x, pB, pA, odd, 0, 0);
+      if (__builtin_expect(partly, 0)) mask(sA, key1);
+      raise(sA, x, pB);
+      stage(NOT_FILED, sB, even + UNITB, x, pA, pB, odd + UNITB, 0, 0);
+      if (__builtin_expect(partly, 0)) mask(sB, key1 + 32);
+      not_numbers(t);
+    };
+    const auto last = [&](int t, unsigned odd) INLINE {
+      barrier();
+      raise(sB, x, pA);
+      weigh(x, pB);
+      multiply(pA, odd);
+      multiply(pB, odd + UNITB);
+      not_numbers(t);
+    };
+    // The same where tiles up to t + 3 are cached and seen by all rows as a whole: nothing to ask for.
+    const int plain_hi = whole_hi < wg_free ? whole_hi : wg_free;
+    const int n_plain = plain_hi > key_of(0) ? (plain_hi - key_of(0) + KEYS * (H - 1)) / (KEYS * H) : 0;
+    GlobalBytes next_kc = (GlobalBytes)a.q4.k_codes + (rows0 + key_of(3)) * (D / 2), next_ks = (GlobalBytes)a.q4.k_scales + (rows0 + key_of(3)) * (D / 32);
+    GlobalBytes next_vc = (GlobalBytes)a.q4.v_codes + (rows0 + key_of(2)) * (D / 2), next_vs = (GlobalBytes)a.q4.v_scales + (rows0 + key_of(2)) * (D / 32);
+    const auto plain_step = [&](unsigned odd) INLINE {
+      const unsigned even = TILEB - odd;
+      barrier();
+      raise(sB, x, pA);
+      stage(FILED, sA, even, x, pB, pA, odd, odd, 2 * TILEB + even);
+      take(rk, next_kc + c_off, next_ks + s_off);
+      take(rv, next_vc + c_off, next_vs + s_off);
+      next_kc += KEYS * H * (D / 2);
+      next_ks += KEYS * H * (D / 32);
+      next_vc += KEYS * H * (D / 2);
+      next_vs += KEYS * H * (D / 32);
+      raise(sA, x, pB);
+      stage(NOT_FILED, sB, even + UNITB, x, pA, pB, odd + UNITB, 0, 0);
+    };
+    int t = 0;
+    for (; t + 4 < n_plain; t += 2) {
+      plain_step(0);
+      plain_step(TILEB);
+    }
+    for (; t + 2 < n_tiles; t += 2) {
+      step(t, 0);
+      step(t + 1, TILEB);
+    }
+    if (t + 2 == n_tiles) {
+      step(t, 0);
+      last(t + 1, TILEB);
+    } else if (t < n_tiles) {
+      last(t, 0);
+    }
+    if (H == 2 && n_tiles < most_tiles) barrier();      // (the other half has a tile more)
+
   };
-  const auto last = [&](int t, unsigned odd) {
-    barrier();
-    raise(sB, x, pA);
-    weigh(x, pB);
-    multiply(pA, odd);
-    multiply(pB, odd + UNITB);
-    not_numbers(t);
-  };
-  // The same where tiles up to t + 3 are cached and seen by all rows as a whole: nothing to ask for.
-  const int plain_hi = whole_hi < wg_free ? whole_hi : wg_free;
-  const int n_plain = plain_hi > key_of(0) ? (plain_hi - key_of(0) + KEYS * (H - 1)) / (KEYS * H) : 0;
-  GlobalBytes next_kc = (GlobalBytes)a.q4.k_codes + (rows0 + key_of(3)) * (D / 2), next_ks = (GlobalBytes)a.q4.k_scales + (rows0 + key_of(3)) * (D / 32);
-  GlobalBytes next_vc = (GlobalBytes)a.q4.v_codes + (rows0 + key_of(2)) * (D / 2), next_vs = (GlobalBytes)a.q4.v_scales + (rows0 + key_of(2)) * (D / 32);
-  const auto plain_step = [&](unsigned odd) {
-    const unsigned even = TILEB - odd;
-    barrier();
-    raise(sB, x, pA);
-    stage(FILED, sA, even, x, pB, pA, odd, odd, 2 * TILEB + even);
-    take(rk, next_kc + c_off, next_ks + s_off);
-    take(rv, next_vc + c_off, next_vs + s_off);
-    next_kc += KEYS * H * (D / 2);
-    next_ks += KEYS * H * (D / 32);
-    next_vc += KEYS * H * (D / 2);
-    next_vs += KEYS * H * (D / 32);
-    raise(sA, x, pB);
-    stage(NOT_FILED, sB, even + UNITB, x, pA, pB, odd + UNITB, 0, 0);
-  };
-  int t = 0;
-  for (; t + 4 < n_plain; t += 2) {
-    plain_step(0);
-    plain_step(TILEB);
+  walk(std::integral_constant<bool, false>());
+  __shared__ int lds_wide[8];
+  if (lane == 0) lds_wide[threadIdx.x >> 6] = wide.flags();
+  __syncthreads();
+  int any_wide = 0;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) any_wide |= lds_wide[k];
+  if (__builtin_expect(__builtin_amdgcn_readfirstlane(any_wide) != 0, 0)) {
+    down = any_wide & 2 ? DOWN : 0;
+    walk(std::integral_constant<bool, true>());
   }
-  for (; t + 2 < n_tiles; t += 2) {
-    step(t, 0);
-    step(t + 1, TILEB);
-  }
-  if (t + 2 == n_tiles) {
-    step(t, 0);
-    last(t + 1, TILEB);
-  } else if (t < n_tiles) {
-    last(t, 0);
-  }
-  if (H == 2 && n_tiles < most_tiles) barrier();      // (the other half has a tile more)
 
   // ---- results.  The halves meet: the second hands over (O, m, l), register by register.
   float l[RB];
@@ -498,9 +524,9 @@ __global__ __launch_bounds__(THREADS, 2) void q4_tiles_kernel(Q4Args a, TileDiv 
     if (row >= R) continue;
     const int j = (int)quotient(row, by.G);
     const size_t out = out0 + (size_t)(kvh * g.G + row - j * g.G) * a.q_len + j;
-    const float inv = l[b] == 0.f ? 0.f : 1.f / l[b];
+    const float inv = l[b] == 0.f ? 0.f : 1.f / l[b], up = down ? __builtin_ldexpf(1.f, DOWN) : 1.f;
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt) *(f32x4*)(a.O_sub + out * D + 16 * dt + 4 * j4) = r.o[b][dt] * inv;
+    for (int dt = 0; dt < DT; ++dt) *(f32x4*)(a.O_sub + out * D + 16 * dt + 4 * j4) = r.o[b][dt] * inv * up;
     if (j4 == 0) a.LSE_sub[out] = l[b] == 0.f ? -INFINITY : (r.ref[b] + __builtin_amdgcn_logf(l[b])) * LN2;
   }
 }
@@ -526,8 +552,8 @@ hipError_t launch_phase2_q4_tiles(int dtype, const Q4Args& a, hipStream_t st) {
     if (rows == 256) return a.parts == 2 ? launch_tiles<__bf16, 128, 2, 2, 1>(a, st) : launch_tiles<__bf16, 128, 1, 2, 1>(a, st);
     return a.parts == 2 ? launch_tiles<__bf16, 128, 2, 2, 2>(a, st) : launch_tiles<__bf16, 128, 1, 2, 2>(a, st);
   }
-  if (a.g.d == 64) return rows == 128 ? launch_tiles<float, 64, 3, 1, 1>(a, st) : launch_tiles<float, 64, 3, 1, 2>(a, st);
-  return rows == 128 ? launch_tiles<float, 128, 3, 1, 1>(a, st) : launch_tiles<float, 128, 3, 1, 2>(a, st);
+  if (a.g.d == 64) return rows == 128 ? launch_tiles<float, 64, 2, 1, 1>(a, st) : launch_tiles<float, 64, 2, 1, 2>(a, st);
+  return rows == 128 ? launch_tiles<float, 128, 2, 1, 1>(a, st) : launch_tiles<float, 128, 2, 1, 2>(a, st);
 }
 
 }  // namespace star

@@ -331,7 +331,7 @@ struct Q4Args {
   SplitPlan plan;
   int64_t cache_len;
   int32_t q_len, causal;
-  int32_t parts;          // bf16: bf16 parts a weight is taken in, 1 or 2
+  int32_t parts;          // bf16: fp16 parts a weight is taken in, 1 or 2
   const void* Qq;
   const void* Kn;         // the call's K, V [B, q_len, Hkv, d], which the kernel files; null: the cache holds them, or there are none
   const void* Vn;

@@ -215,7 +215,7 @@ def test_a_serving_run():
             k, e = star_q4.quantise(Yk[0, :at + n, g])
             assert torch.equal(cache.k_codes[0, g, :at + n], k) and torch.equal(cache.k_scales[0, g, :at + n], e)
             v, f = star_q4.quantise(V[0, :at + n, g])
-            A, _, weights, size = star_q4.attend(q[0, :, h], star_q4.values(k, e), star_q4.values(v, f), d ** -0.5, at)
-            bound = weights * (2.0 ** -8 + 2.0 ** -23 * ((d + 4) * size[:, None] + at / 32 + 64)) + A.abs() * 2.0 ** -8
+            A, _, weights, size, total = star_q4.attend(q[0, :, h], star_q4.values(k, e), star_q4.values(v, f), d ** -0.5, at)
+            bound = weights * (2.0 ** -8 + 2.0 ** -23 * ((d + 4) * size[:, None] + at / 32 + 64)) + total * 2.0 ** -35 + A.abs() * 2.0 ** -8
             assert ((out[0, :, h].double() - A).abs() <= bound).all()
         at += n

@@ -1,9 +1,12 @@
 """A cache held in four bits: rows filed and read, exactly, and phase 2 over it, against 64 bits (oracle/star_q4.py).
 
 Bounds.  Four-bit values are exact in the products.  A logit is a sum of d products held in 32 bits, and its argument of the
-exponential two roundings more: off by (d + 4) 2^-24 of sum |q k| scale, at most.  Weights are rounded to half a step of bf16 (2^-8), of
-two bf16 parts (2^-16) or of fp32 (2^-24); their sums over n keys round n / 32 + 64 times.  A relative error of every weight
-moves an output by that times sum p |v|, twice, because the sum of the weights has it too."""
+exponential two roundings more: off by (d + 4) 2^-24 of sum |q k| scale, at most.  Weights are rounded to half a step of bf16 (2^-8) at most, of
+two parts (2^-16) or of fp32 (2^-24); their sums over n keys round n / 32 + 64 times.  A relative error of every weight
+moves an output by that times sum p |v|, twice, because the sum of the weights has it too.
+fp16 has a least step, 2^-24, and a row's largest weight is 2^10 or more when it is taken (2^(TOP + 1 - 4) to half of that in the row-tiled
+kernel, 2^13.5 in the other): a weight may be off by half that step, 2^-25 / 2^10 of the largest, which is no more than the sum by which
+outputs are divided.  Over all keys that is 2^-35 sum |v| at most.  (Keys whose values fp16 does not hold are weighted in bf16.)"""
 import math
 
 import pytest
@@ -19,11 +22,11 @@ def _randn(gen, dtype, *size):
     return torch.randn(size, generator=gen).to(torch.float32 if dtype == "fp32" else torch.bfloat16).cuda()
 
 
-def _bound(dtype, d, n, size, weights, parts):
-    """Of an output whose rows have `size` = sum |q k| scale and `weights` = sum p |v|."""
+def _bound(dtype, d, n, size, weights, total, parts):
+    """Of an output whose rows have `size` = sum |q k| scale, `weights` = sum p |v| and `total` = sum |v|."""
     u = 2.0 ** -24
     step = u if dtype == "fp32" else 2.0 ** -16 if parts == 2 else 2.0 ** -8
-    return weights * (step + 2 * u * ((d + 4) * size[:, None] + n / 32 + 64)) + 1e-30
+    return weights * (step + 2 * u * ((d + 4) * size[:, None] + n / 32 + 64)) + total * 2.0 ** -35 + 1e-30
 
 
 class Call:
@@ -77,20 +80,20 @@ class Call:
 
     def check_O(self, tensors, few=4):
         for b, h in self.heads(few):
-            A, lse, weights, size = self.exact(tensors, b, h)
-            bound = _bound(self.dtype, self.dims[3], self.cached + self.q, size, weights, 1)
+            A, lse, weights, size, total = self.exact(tensors, b, h)
+            bound = _bound(self.dtype, self.dims[3], self.cached + self.q, size, weights, total, 1)
             self.near(self.O[b, :, h], A, bound + A.abs() * (2.0 ** -24 if self.dtype == "fp32" else 2.0 ** -8), (b, h))
 
     def check_pair(self, tensors, A, LSE, append, few=4, lo=0, hi=None):
         for b, h in self.heads(few):
-            want, lse, weights, size = self.exact(tensors, b, h, append, lo, hi)
+            want, lse, weights, size, total = self.exact(tensors, b, h, append, lo, hi)
             n = self.cached + self.q
             empty = lse == -math.inf
             assert torch.equal(LSE[b, h] == -math.inf, empty) and (A[b, h][empty] == 0).all()
             seen = ~empty
             if not seen.any():
                 continue
-            self.near(A[b, h][seen], want[seen], (_bound(self.dtype, self.dims[3], n, size, weights, 2) + want.abs() * 2.0 ** -24)[seen], (b, h))
+            self.near(A[b, h][seen], want[seen], (_bound(self.dtype, self.dims[3], n, size, weights, total, 2) + want.abs() * 2.0 ** -24)[seen], (b, h))
             self.near(LSE[b, h][seen], lse[seen], (2.0 ** -24 * (2 * (self.dims[3] + 4) * size + n / 32 + 64 + 8 * lse.abs()))[seen], (b, h, "lse"))
 
 
@@ -283,6 +286,52 @@ def test_values_and_queries_far_from_one():
     sa.phase2_q4(c.shape, 400, c.Q, c.K, c.V, c.cache, c.O, c.ws)
     torch.cuda.synchronize()
     assert all(torch.equal(x, y) for x, y in zip(c.tensors(), want))
+    c.check_O(want, few=8)
+
+
+@pytest.mark.parametrize("at", ["first", "middle", "last", "new"])
+@pytest.mark.parametrize("dtype,Hq,Hkv,d,L,q", [("bf16", 8, 2, 128, 900, 3), ("bf16", 8, 2, 128, 900, 7), ("bf16", 8, 2, 128, 2000, 70),
+                                                ("bf16", 32, 8, 128, 3000, 128), ("fp32", 4, 2, 64, 900, 4), ("fp32", 8, 2, 128, 900, 40)])
+def test_values_that_fp16_does_not_hold(dtype, Hq, Hkv, d, L, q, at):
+    """Units of V past 2^13 and below 2^-23, in cached rows and in the call's own; a key whose group is NaN among the cached."""
+    c = Call(dtype, 1, Hq, Hkv, d, L, q, seed=10)
+    print(f"{dtype} {Hq}/{Hkv} L={L} q={q} {at}", flush=True)
+    if at == "new":
+        c.V[:, 0, 0] *= 2.0 ** 20
+        c.V[:, q - 1, 1] *= 2.0 ** -60
+    else:
+        row = {"first": 0, "middle": L // 2, "last": L - 1}[at]
+        c.cache.v_scales[0, 0, row] += 30
+        c.cache.v_scales[0, 1, row, 1] -= 50
+    want = c.appended()
+    sa.phase2_q4(c.shape, L, c.Q, c.K, c.V, c.cache, c.O, c.ws)
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(c.tensors(), want))
+    c.check_O(want, few=8)
+    A, LSE = torch.empty((1, Hq, q, d)).cuda(), torch.empty((1, Hq, q)).cuda()
+    sa.phase2_q4_partial(c.shape, L, c.Q, c.cache, A, LSE, c.ws, Kq=c.K, Vq=c.V)
+    torch.cuda.synchronize()
+    c.check_pair(want, A, LSE, True, few=8)
+    if at != "new":
+        c.cache.v_scales[0, 0, row, 0], c.cache.k_scales[0, 1, row, 0] = 255, 255
+        sa.phase2_q4(c.shape, L, c.Q, c.K, c.V, c.cache, c.O, c.ws)
+        torch.cuda.synchronize()
+        G = Hq // Hkv
+        nan = c.O[0].isnan()
+        assert nan[:, :G, :32].all() and not nan[:, :G, 32:].any() and nan[:, G:2 * G].all() and not nan[:, 2 * G:].any()
+
+
+@pytest.mark.parametrize("dtype,Hq,Hkv,d,L,q", [("bf16", 8, 2, 128, 900, 3), ("bf16", 8, 2, 128, 6000, 70), ("fp32", 8, 2, 128, 900, 40)])
+def test_scores_that_rise_all_along(dtype, Hq, Hkv, d, L, q):
+    """Each key's logit above the one before, by 2^9 in all: the references move, everywhere, and what was summed up before fades."""
+    c = Call(dtype, 1, Hq, Hkv, d, L, q, seed=11)
+    c.Q.fill_(1.0)
+    K = (torch.arange(L)[:, None] / L * 45 * torch.ones(d))[None, None].expand(1, Hkv, L, d)
+    codes, scales = star_q4.quantise(K)
+    c.cache.k_codes[:, :, :L], c.cache.k_scales[:, :, :L] = codes.cuda(), scales.cuda()
+    want = c.appended()
+    sa.phase2_q4(c.shape, L, c.Q, c.K, c.V, c.cache, c.O, c.ws)
+    torch.cuda.synchronize()
     c.check_O(want, few=8)
 
 

@@ -20,7 +20,7 @@ def test_codes_and_units():
 def test_largest_element_decides():
     for most, unit in ((3.5, 0), (6.99, 0), (7.0, 1), (3.49, -1), (1.0, -2), (1.75, -1), (1.7499, -2)):
         assert star_q4.quantise(_group(most))[1].item() == 127 + unit, most
-    assert star_q4.quantise(_group(0.0))[1].item() == 2
+    assert star_q4.quantise(_group(0.0))[1].item() == 127 and star_q4.quantise(_group(-0.0, 0.0))[1].item() == 127
     assert star_q4.quantise(_group(1e-40))[1].item() == 2
     codes, e = star_q4.quantise(_group(3.4e38))
     assert e.item() == 252 and star_q4.values(codes, e)[0, 0].item() == 6 * 2.0 ** 125
@@ -45,10 +45,11 @@ def test_error_of_a_group():
 def test_attention_of_two_keys():
     Q = torch.tensor([[2.0, 0.0], [0.0, 1.0]])
     K, V = torch.tensor([[1.0, 0.0], [0.0, 3.0]]), torch.tensor([[1.0, 0.0], [0.0, 1.0]])
-    A, lse, size, most = star_q4.attend(Q, K, V, 0.5, cache_len=0)
+    A, lse, size, most, total = star_q4.attend(Q, K, V, 0.5, cache_len=0)
     assert torch.allclose(A[0], torch.tensor([1.0, 0.0]).double()) and lse[0].item() == 1.0            # the first sees itself alone
     w = torch.softmax(torch.tensor([0.0, 1.5]).double(), 0)
     assert torch.allclose(A[1], w) and torch.allclose(size[1], w) and most.tolist() == [1.0, 1.5]
+    assert total.tolist() == [[1.0, 0.0], [1.0, 1.0]]
 
 
 def test_norm_and_rotation_by_hand():
