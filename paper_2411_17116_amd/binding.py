@@ -97,22 +97,28 @@ class Rotary:
         for w in (q_norm, k_norm):
             if w is not None and w.dim() != 1:
                 raise ValueError("norm weights are [head_dim]")
+        norms = {(w.shape[0], w.element_size()) for w in (q_norm, k_norm) if w is not None}
+        if len(norms) > 1:
+            raise ValueError("norm weights are [head_dim] in the storage dtype")
         self.tensors = (q_norm, k_norm, positions)
-        self.frequencies = None if axis is None else len(axes)
         self.c = StarRotary(float(rope_theta), int(pos0), _pointer(positions, "positions", torch.int64), _pointer(q_norm, "q_norm"),
                             _pointer(k_norm, "k_norm"), float(eps), n_axes, (ctypes.c_uint8 * 64)(*axes))
+        size, item = next(iter(norms), (0, 0))
+        tokens = (0, 0) if positions is None else tuple(positions.shape[:2])
+        self.held = _HeldRotary(self.c, size, item, 0 if axis is None else len(axes), *tokens)
 
+
+class _HeldRotary(ctypes.Structure):
+    """A call's checks of it are made where its arguments are read: the extension module, or _CtypesCalls."""
+    _fields_ = [("c", StarRotary), ("norm", ctypes.c_int32), ("item", ctypes.c_int32), ("frequencies", ctypes.c_int32),
+                ("batch", ctypes.c_int32), ("tokens", ctypes.c_int64)]
 
     def of(self, shape: StarShape, n_tokens: int) -> StarRotary:
-        """The struct, for a call of that shape."""
-        q_norm, k_norm, positions = self.tensors
-        d, size = shape.head_dim, 4 if shape.dtype == F32 else 2
-        for w in (q_norm, k_norm):
-            if w is not None and (w.shape[0] != d or w.element_size() != size):
-                raise ValueError("norm weights are [head_dim] in the storage dtype")
-        if positions is not None and tuple(positions.shape[:2]) != (shape.batch, n_tokens):
-            raise ValueError(f"positions of {tuple(positions.shape[:2])} tokens given, {(shape.batch, n_tokens)} wanted")
-        if self.frequencies not in (None, d // 2):
+        if self.norm and (self.norm != shape.head_dim or self.item != (4 if shape.dtype == F32 else 2)):
+            raise ValueError("norm weights are [head_dim] in the storage dtype")
+        if self.c.positions and (self.batch, self.tokens) != (shape.batch, n_tokens):
+            raise ValueError("positions of other tokens than the call's")
+        if self.frequencies and 2 * self.frequencies != shape.head_dim:
             raise ValueError("an axis for each of the d / 2 frequencies is wanted")
         return self.c
 
@@ -129,15 +135,18 @@ class Q4Cache:
     def __init__(self, shape: StarShape, k_codes, k_scales, v_codes, v_scales):
         rows = (shape.batch, shape.n_kv_heads, shape.cache_capacity)
         sizes = {"codes": rows + (shape.head_dim // 2,), "scales": rows + (shape.head_dim // 32,)}
-        self.rows, self.head_dim = rows, shape.head_dim
         self.k_codes, self.k_scales, self.v_codes, self.v_scales = k_codes, k_scales, v_codes, v_scales
         self.c = StarQ4(*(_pointer(getattr(self, n), n, torch.uint8, sizes[n[2:]]) for n, _ in StarQ4._fields_))
+        self.held = _HeldQ4(self.c, shape.batch, shape.n_kv_heads, shape.head_dim, 0, shape.cache_capacity)
 
+
+class _HeldQ4(ctypes.Structure):
+    _fields_ = [("c", StarQ4), ("batch", ctypes.c_int32), ("heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("unused", ctypes.c_int32), ("rows", ctypes.c_int64)]
 
     def of(self, shape: StarShape) -> StarQ4:
-        """The struct, for a call of that shape."""
-        if self.rows != (shape.batch, shape.n_kv_heads, shape.cache_capacity) or self.head_dim != shape.head_dim:
-            raise ValueError(f"a four-bit cache of {self.rows} rows of {self.head_dim} given to a call of another shape")
+        if (self.batch, self.heads, self.head_dim, self.rows) != (shape.batch, shape.n_kv_heads, shape.head_dim, shape.cache_capacity):
+            raise ValueError("a four-bit cache of another shape than the call's")
         return self.c
 
 
@@ -252,16 +261,15 @@ def _bind(lib) -> None:
 class _CtypesCalls:
     """The extension module's calls by ctypes alone: same arguments, same refusals."""
     # what follows the shape and precedes the stream: t a tensor's address, w and its bytes, q behind its shape[1],
-    # m behind its shape[0] and shape[3]; i and d numbers; r a struct or None
+    # m behind its shape[0] and shape[3]; i and d numbers; 4 a four-bit cache
     _KINDS = {"phase1": "tttttttw", "phase1_anchor": "itttttttttw", "phase1_rope": "ditttttttw", "phase2": "iqtttttttw",
               "phase2_rope": "diiqtttttttw", "phase2_static": "iqttttt", "phase2_partial": "iqttttttw", "merge": "mtttt"}
-    _Q4_KINDS = {"qk_norm_rope": "ritttt", "phase1_norm_rope": "rtttttttw", "phase2_norm_rope": "riqtttttttw",
-                 "phase2_q4": "riqttrtttw", "phase2_q4_partial": "iqttrttw"}
+    _Q4_KINDS = {"phase2_q4_partial": "iqtt4ttw"}
 
     def __init__(self, lib):
         self._rope, kinds = lib.star_attn_rope, dict(self._KINDS)
         if hasattr(lib, "star_attn_phase2_q4"):
-            self._q4_store, self._q4_load = lib.star_attn_q4_store, lib.star_attn_q4_load
+            self._lib = lib
             kinds.update(self._Q4_KINDS)
         for name, kinds in kinds.items():
             setattr(self, name, self._entry(getattr(lib, "star_attn_" + name), kinds))
@@ -274,10 +282,6 @@ class _CtypesCalls:
             raise ValueError("star_attn tensors must be contiguous")
         return t.data_ptr()
 
-    @staticmethod
-    def _struct(x):
-        return None if x is None else ctypes.byref(x)
-
     def _entry(self, fn, kinds):
         def call(shape, *args):
             *values, stream = args
@@ -289,7 +293,7 @@ class _CtypesCalls:
                     out.append(x.shape[1])
                 elif kind == "m":
                     out += [x.shape[0], x.shape[3]]
-                out.append(x if kind in "id" else self._struct(x) if kind == "r" else self._address(x))
+                out.append(x if kind in "id" else ctypes.byref(x.of(shape)) if kind == "4" else self._address(x))
                 if kind == "w":
                     out.append(0 if x is None else x.numel() * x.element_size())
             return fn(*out, stream)
@@ -299,11 +303,36 @@ class _CtypesCalls:
         return self._rope(ctypes.byref(shape), X.shape[2], X.shape[1], pos0, theta, self._address(X), self._address(Y), stream)
 
 
+    def qk_norm_rope(self, shape, tokens, rotary, Q, K, Yq, Yk, stream):
+        return self._lib.star_attn_qk_norm_rope(ctypes.byref(shape), ctypes.byref(rotary.of(shape, tokens)), tokens,
+                                                *map(self._address, (Q, K, Yq, Yk)), stream)
+
+    def phase1_norm_rope(self, shape, rotary, Q, K, V, O, LSE, Kc, Vc, ws, stream):
+        return self._lib.star_attn_phase1_norm_rope(ctypes.byref(shape), ctypes.byref(rotary.of(shape, shape.ctx_len)),
+                                                    *map(self._address, (Q, K, V, O, LSE, Kc, Vc, ws)), _nbytes(ws), stream)
+
+    def phase2_norm_rope(self, shape, cached, Q, rotary, K, V, Kc, Vc, O_part, LSE_part, O, ws, stream):
+        q = Q.shape[1]
+        return self._lib.star_attn_phase2_norm_rope(ctypes.byref(shape), ctypes.byref(rotary.of(shape, q)), cached, q,
+                                                    *map(self._address, (Q, K, V, Kc, Vc, O_part, LSE_part, O, ws)), _nbytes(ws), stream)
+
     def q4_store(self, shape, row, rows, K, V, plain_row, cache, stream):
-        return self._q4_store(ctypes.byref(shape), row, rows, self._address(K), self._address(V), K.shape[2], plain_row, self._struct(cache), stream)
+        return self._lib.star_attn_q4_store(ctypes.byref(shape), row, rows, self._address(K), self._address(V), K.shape[2], plain_row,
+                                            ctypes.byref(cache.of(shape)), stream)
 
     def q4_load(self, shape, row, rows, K, V, plain_row, cache, stream):
-        return self._q4_load(ctypes.byref(shape), row, rows, self._struct(cache), self._address(K), self._address(V), K.shape[2], plain_row, stream)
+        return self._lib.star_attn_q4_load(ctypes.byref(shape), row, rows, ctypes.byref(cache.of(shape)), self._address(K), self._address(V),
+                                           K.shape[2], plain_row, stream)
+
+    def phase2_q4(self, shape, cached, Q, rotary, K, V, cache, O_part, LSE_part, O, ws, stream):
+        q = Q.shape[1]
+        rotary = None if rotary is None else ctypes.byref(rotary.of(shape, q))
+        return self._lib.star_attn_phase2_q4(ctypes.byref(shape), rotary, cached, q, *map(self._address, (Q, K, V)), ctypes.byref(cache.of(shape)),
+                                             *map(self._address, (O_part, LSE_part, O, ws)), _nbytes(ws), stream)
+
+
+def _nbytes(t):
+    return 0 if t is None else t.numel() * t.element_size()
 
 
 def _calls():
@@ -449,19 +478,19 @@ def qk_norm_rope(shape: StarShape, rotary: Rotary, Q, K, Yq, Yk, stream=None) ->
     """star_attn_qk_norm_rope: queries Q and keys K [B, T, H, d] (either may be None) normed per head and rotated into
     Yq and Yk (which may be Q and K)."""
     tokens = (Q if Q is not None else K).shape[1]
-    _check(_calls().qk_norm_rope(shape, rotary.of(shape, tokens), tokens, Q, K, Yq, Yk, _stream(stream)))
+    _check(_calls().qk_norm_rope(shape, tokens, rotary.held, Q, K, Yq, Yk, _stream(stream)))
 
 
 def phase1_norm_rope(shape: StarShape, rotary: Rotary, Q, K, V, O_ctx, K_cache, V_cache, LSE_ctx=None, workspace=None,
                      stream=None) -> None:
     """star_attn_phase1_norm_rope: phase 1 on queries (normed and rotated in place) and keys as they are projected."""
-    _check(_calls().phase1_norm_rope(shape, rotary.of(shape, shape.ctx_len), Q, K, V, O_ctx, LSE_ctx, K_cache, V_cache, workspace, _stream(stream)))
+    _check(_calls().phase1_norm_rope(shape, rotary.held, Q, K, V, O_ctx, LSE_ctx, K_cache, V_cache, workspace, _stream(stream)))
 
 
 def phase2_norm_rope(shape: StarShape, rotary: Rotary, cache_len: int, Qq, Kq, Vq, K_cache, V_cache, O, workspace,
                      O_part=None, LSE_part=None, stream=None) -> None:
     """star_attn_phase2_norm_rope: phase 2 on queries (normed and rotated in place) and keys as they are projected."""
-    _check(_calls().phase2_norm_rope(shape, rotary.of(shape, Qq.shape[1]), int(cache_len), Qq, Kq, Vq, K_cache, V_cache, O_part, LSE_part, O,
+    _check(_calls().phase2_norm_rope(shape, int(cache_len), Qq, rotary.held, Kq, Vq, K_cache, V_cache, O_part, LSE_part, O,
                                      workspace, _stream(stream)))
 
 
@@ -485,13 +514,13 @@ def alloc_q4_workspace(shape: StarShape, max_q_len: int, device="cuda") -> torch
 def q4_store(shape: StarShape, first_row: int, n_rows: int, K, V, cache: Q4Cache, plain_row=None, stream=None) -> None:
     """star_attn_q4_store: rows [plain_row, plain_row + n_rows) of K and V [B, Hkv, rows, d] (by default those of the same
     numbers) into rows [first_row, first_row + n_rows) of the cache."""
-    _check(_calls().q4_store(shape, int(first_row), int(n_rows), K, V, int(first_row if plain_row is None else plain_row), cache.of(shape),
+    _check(_calls().q4_store(shape, int(first_row), int(n_rows), K, V, int(first_row if plain_row is None else plain_row), cache.held,
                              _stream(stream)))
 
 
 def q4_load(shape: StarShape, first_row: int, n_rows: int, cache: Q4Cache, K, V, plain_row=None, stream=None) -> None:
     """star_attn_q4_load: the same rows of the cache into K and V, as what their codes stand for."""
-    _check(_calls().q4_load(shape, int(first_row), int(n_rows), K, V, int(first_row if plain_row is None else plain_row), cache.of(shape),
+    _check(_calls().q4_load(shape, int(first_row), int(n_rows), K, V, int(first_row if plain_row is None else plain_row), cache.held,
                             _stream(stream)))
 
 
@@ -499,13 +528,13 @@ def phase2_q4(shape: StarShape, cache_len: int, Qq, Kq, Vq, cache: Q4Cache, O, w
               O_part=None, LSE_part=None, stream=None) -> None:
     """star_attn_phase2_q4: files Kq/Vq in the four-bit cache at cache_len, then attends to all it holds; with `rotary`, Qq
     (in place) and Kq are normed and rotated first."""
-    _check(_calls().phase2_q4(shape, None if rotary is None else rotary.of(shape, Qq.shape[1]), int(cache_len), Qq, Kq, Vq, cache.of(shape), O_part, LSE_part, O,
+    _check(_calls().phase2_q4(shape, int(cache_len), Qq, None if rotary is None else rotary.held, Kq, Vq, cache.held, O_part, LSE_part, O,
                               workspace, _stream(stream)))
 
 
 def phase2_q4_partial(shape: StarShape, cache_len: int, Qq, cache: Q4Cache, A, LSE, workspace, Kq=None, Vq=None, stream=None) -> None:
     """star_attn_phase2_q4_partial: one host's pair (A, LSE) over a four-bit cache (see phase2_partial)."""
-    _check(_calls().phase2_q4_partial(shape, int(cache_len), Qq, Kq, Vq, cache.of(shape), A, LSE, workspace, _stream(stream)))
+    _check(_calls().phase2_q4_partial(shape, int(cache_len), Qq, Kq, Vq, cache.held, A, LSE, workspace, _stream(stream)))
 
 
 def phase2_q4_plan(shape: StarShape, cache_len: int, q_len: int, want_parts: bool = False) -> PlanInfo:

@@ -91,8 +91,25 @@ struct Args {
     if (v->len != (Py_ssize_t)sizeof(Record)) { fail(PyExc_TypeError, what); return nullptr; }
     return (const Record*)v->buf;
   }
-  const star_attn_rotary* rotary() { return record<star_attn_rotary>("a Rotary is wanted"); }
-  const star_attn_q4_cache* q4() { return record<star_attn_q4_cache>("a Q4Cache is wanted"); }
+  // The binding's Rotary and Q4Cache hold the struct and what their tensors' sizes were: those of the call are wanted.
+  const star_attn_rotary* rotary(const star_attn_shape* s, int64_t tokens) {
+    struct Held { star_attn_rotary r; int32_t norm, item, frequencies, batch; int64_t tokens; };
+    const Held* h = record<Held>("a Rotary is wanted");
+    if (!h || !s) return nullptr;
+    if (h->norm && (h->norm != s->head_dim || h->item != (s->dtype == STAR_ATTN_F32 ? 4 : 2)))
+      fail(PyExc_ValueError, "norm weights are [head_dim] in the storage dtype");
+    if (h->r.positions && (h->batch != s->batch || h->tokens != tokens)) fail(PyExc_ValueError, "positions of other tokens than the call's");
+    if (h->frequencies && 2 * h->frequencies != s->head_dim) fail(PyExc_ValueError, "an axis for each of the d / 2 frequencies is wanted");
+    return &h->r;
+  }
+  const star_attn_q4_cache* q4(const star_attn_shape* s) {
+    struct Held { star_attn_q4_cache c; int32_t batch, heads, d, unused; int64_t rows; };
+    const Held* h = record<Held>("a Q4Cache is wanted");
+    if (!h || !s) return nullptr;
+    if (h->batch != s->batch || h->heads != s->n_kv_heads || h->d != s->head_dim || h->rows != s->cache_capacity)
+      fail(PyExc_ValueError, "a four-bit cache of another shape than the call's");
+    return &h->c;
+  }
   int64_t integer() {
     PyObject* o = next();
     if (!o) return 0;
@@ -301,12 +318,12 @@ FASTCALL(rope) {
   return finish(a, (const void*)lib.rope, [&] { return lib.rope(s, (int32_t)heads, tokens, pos0, theta, X, Y, st); });
 }
 
-// qk_norm_rope(shape, rotary, n_tokens, Q, K, Yq, Yk, stream)
+// qk_norm_rope(shape, n_tokens, rotary, Q, K, Yq, Yk, stream)
 FASTCALL(qk_norm_rope) {
   Args a(args, n, 8);
   const star_attn_shape* s = a.shape();
-  const star_attn_rotary* r = a.rotary();
   const int64_t tokens = a.integer();
+  const star_attn_rotary* r = a.rotary(s, tokens);
   void *Q = a.pointer(), *K = a.pointer(), *Yq = a.pointer(), *Yk = a.pointer(), *st = a.stream();
   return finish(a, (const void*)q4lib.qk_norm_rope, [&] { return q4lib.qk_norm_rope(s, r, tokens, Q, K, Yq, Yk, st); });
 }
@@ -314,21 +331,22 @@ FASTCALL(qk_norm_rope) {
 FASTCALL(phase1_norm_rope) {
   Args a(args, n, 11);
   const star_attn_shape* s = a.shape();
-  const star_attn_rotary* r = a.rotary();
+  const star_attn_rotary* r = a.rotary(s, s ? s->ctx_len : 0);
   void *Q = a.pointer(), *K = a.pointer(), *V = a.pointer(), *O = a.pointer(), *L = a.pointer(), *Kc = a.pointer(), *Vc = a.pointer();
   int64_t ws_n;
   void *ws = a.sized(-1, &ws_n), *st = a.stream();
   return finish(a, (const void*)q4lib.phase1_norm_rope,
                 [&] { return q4lib.phase1_norm_rope(s, r, Q, K, V, O, (float*)L, Kc, Vc, ws, (size_t)ws_n, st); });
 }
-// phase2_norm_rope(shape, rotary, cache_len, Qq, Kq, Vq, K_cache, V_cache, O_part, LSE_part, O, workspace, stream)
+// phase2_norm_rope(shape, cache_len, Qq, rotary, Kq, Vq, K_cache, V_cache, O_part, LSE_part, O, workspace, stream)
 FASTCALL(phase2_norm_rope) {
   Args a(args, n, 13);
   const star_attn_shape* s = a.shape();
-  const star_attn_rotary* r = a.rotary();
   const int64_t cached = a.integer();
   int64_t q, ws_n;
-  void *Q = a.sized(1, &q), *K = a.pointer(), *V = a.pointer(), *Kc = a.pointer(), *Vc = a.pointer(), *Op = a.pointer(),
+  void* Q = a.sized(1, &q);
+  const star_attn_rotary* r = a.rotary(s, q);
+  void *K = a.pointer(), *V = a.pointer(), *Kc = a.pointer(), *Vc = a.pointer(), *Op = a.pointer(),
        *Lp = a.pointer(), *O = a.pointer(), *ws = a.sized(-1, &ws_n), *st = a.stream();
   return finish(a, (const void*)q4lib.phase2_norm_rope, [&] {
     return q4lib.phase2_norm_rope(s, r, cached, q, Q, K, V, Kc, Vc, (float*)Op, (float*)Lp, O, ws, (size_t)ws_n, st);
@@ -342,7 +360,7 @@ PyObject* q4_rows(Args& a, const void* entry, Call call) {
   int64_t plain_rows;
   void *K = a.sized(2, &plain_rows), *V = a.pointer();
   const int64_t plain_row = a.integer();
-  const star_attn_q4_cache* c = a.q4();
+  const star_attn_q4_cache* c = a.q4(s);
   void* st = a.stream();
   return finish(a, entry, [&] { return call(s, row, rows, K, V, plain_rows, plain_row, c, st); });
 }
@@ -356,15 +374,16 @@ FASTCALL(q4_load) {
                  [](const star_attn_shape* s, int64_t row, int64_t rows, void* K, void* V, int64_t plain_rows, int64_t plain_row,
                     const star_attn_q4_cache* c, void* st) { return q4lib.q4_load(s, row, rows, c, K, V, plain_rows, plain_row, st); });
 }
-// phase2_q4(shape, rotary, cache_len, Qq, Kq, Vq, cache, O_part, LSE_part, O, workspace, stream)
+// phase2_q4(shape, cache_len, Qq, rotary, Kq, Vq, cache, O_part, LSE_part, O, workspace, stream)
 FASTCALL(phase2_q4) {
   Args a(args, n, 12);
   const star_attn_shape* s = a.shape();
-  const star_attn_rotary* r = a.rotary();
   const int64_t cached = a.integer();
   int64_t q, ws_n;
-  void *Q = a.sized(1, &q), *K = a.pointer(), *V = a.pointer();
-  const star_attn_q4_cache* c = a.q4();
+  void* Q = a.sized(1, &q);
+  const star_attn_rotary* r = a.rotary(s, q);
+  void *K = a.pointer(), *V = a.pointer();
+  const star_attn_q4_cache* c = a.q4(s);
   void *Op = a.pointer(), *Lp = a.pointer(), *O = a.pointer(), *ws = a.sized(-1, &ws_n), *st = a.stream();
   return finish(a, (const void*)q4lib.phase2_q4,
                 [&] { return q4lib.phase2_q4(s, r, cached, q, Q, K, V, c, (float*)Op, (float*)Lp, O, ws, (size_t)ws_n, st); });
@@ -376,7 +395,7 @@ FASTCALL(phase2_q4_partial) {
   const int64_t cached = a.integer();
   int64_t q, ws_n;
   void *Q = a.sized(1, &q), *K = a.pointer(), *V = a.pointer();
-  const star_attn_q4_cache* c = a.q4();
+  const star_attn_q4_cache* c = a.q4(s);
   void *A = a.pointer(), *L = a.pointer(), *ws = a.sized(-1, &ws_n), *st = a.stream();
   return finish(a, (const void*)q4lib.phase2_q4_partial,
                 [&] { return q4lib.phase2_q4_partial(s, cached, q, Q, K, V, c, (float*)A, (float*)L, ws, (size_t)ws_n, st); });

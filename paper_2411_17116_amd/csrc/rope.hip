@@ -72,19 +72,21 @@ struct RopeArgs {
 
 // What a launch does beyond that.
 enum { TURN = 0, NORM = 1, NORM_Q4 = 2 };
-struct MoreArgs {
+struct NormArgs {
   const int64_t* positions;     // [B, T, n_axes] or null: token t at pos0 + t
   const void* q_norm;           // [d] or null
   const void* k_norm;
-  float eps;
-  int32_t n_axes;
   uint64_t axis[2];             // two bits per frequency
-  int64_t k_batch, k_row, k_head;     // strides of Kc in elements (NORM; V's are the cache's)
-  Q4Rows q4;                    // NORM_Q4: where K and V go instead
+  float eps;
+  int16_t n_axes, cached;       // cached: keys go to rows of a cache (V's), else Kc is [B, T, Hkv, d]
+};
+struct NormQ4Args : NormArgs {
+  Q4Rows q4;                    // where K and V go
 };
 struct NoMore {};
-template <int MODE> struct More { typedef MoreArgs type; };
+template <int MODE> struct More { typedef NormArgs type; };
 template <> struct More<TURN> { typedef NoMore type; };
+template <> struct More<NORM_Q4> { typedef NormQ4Args type; };
 
 template <typename T, int half, int TT, int MODE>
 __global__ __launch_bounds__(THREADS) void rope_kernel(RopeArgs a, typename More<MODE>::type more) {
@@ -140,7 +142,7 @@ __global__ __launch_bounds__(THREADS) void rope_kernel(RopeArgs a, typename More
         src = (const T*)(v ? a.V : a.K) + ((size_t)tok * a.Hkv + g) * d + c;
         dst[u] = (T*)(v ? a.Vc : a.Kc) + cache0 + (size_t)g * a.cap * d;
         if constexpr (MODE == NORM)
-          if (!v) dst[u] = (T*)a.Kc + beta * more.k_batch + t * more.k_row + g * more.k_head + c;
+          if (!v && !more.cached) dst[u] = (T*)a.Kc + ((size_t)tok * a.Hkv + g) * d + c;
       }
       lo[u] = *(const vec*)src;
       hi[u] = *(const vec*)(src + half);
@@ -246,13 +248,11 @@ hipError_t launch_qk(int dtype, const Geom& g, const QkArgs& q, hipStream_t st) 
   a.n_tokens = (uint32_t)q.n_tokens; a.total = (uint32_t)total;
   a.cap = g.cap; a.dst_row = q.dst_row; a.pos0 = q.pos0; a.log2_theta = log2(q.theta);
   a.clear = q.clear;
-  MoreArgs m;
-  m.positions = q.positions; m.q_norm = q.q_norm; m.k_norm = q.k_norm; m.eps = q.eps; m.n_axes = q.n_axes;
-  m.axis[0] = q.axis[0]; m.axis[1] = q.axis[1]; m.q4 = q.q4;
-  if (q.q4.k_codes) return launch<NORM_Q4>(dtype, g.d, a, m, st);
-  if (q.cached) { m.k_batch = (int64_t)g.Hkv * g.cap * g.d; m.k_row = g.d; m.k_head = g.cap * g.d; a.Kc = (char*)q.Yk + q.dst_row * g.d * (dtype == 0 ? 4 : 2); }
-  else { m.k_batch = q.n_tokens * g.Hkv * g.d; m.k_row = (int64_t)g.Hkv * g.d; m.k_head = g.d; }
-  return launch<NORM>(dtype, g.d, a, m, st);
+  NormQ4Args m;
+  m.positions = q.positions; m.q_norm = q.q_norm; m.k_norm = q.k_norm; m.eps = q.eps; m.n_axes = (int16_t)q.n_axes;
+  m.axis[0] = q.axis[0]; m.axis[1] = q.axis[1]; m.cached = (int16_t)q.cached;
+  m.q4 = q.q4;
+  return q.q4.k_codes ? launch<NORM_Q4>(dtype, g.d, a, m, st) : launch<NORM>(dtype, g.d, a, m, st);
 }
 
 }  // namespace star
