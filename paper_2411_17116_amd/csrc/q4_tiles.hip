@@ -54,7 +54,8 @@ __global__ __launch_bounds__(THREADS, 2) void q4_tiles_kernel(Q4Args a, TileDiv 
   __shared__ uint32_t lds_e[H][2][KEYS];                                      // exponents of V, of tiles that not every row sees as a whole
   const Geom& g = a.g;
   const int ring = H == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 8), tid = threadIdx.x & (64 * W - 1);
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, qc = lane & 15, j4 = lane >> 4;
+  // Wavefronts w and w + 4 share a SIMD: the halves number their rows' from different ones, so that those of few rows keep all four busy.
+  const int wave = (__builtin_amdgcn_readfirstlane(tid >> 6) + (ring ? 2 : 0)) & (W - 1), lane = tid & 63, qc = lane & 15, j4 = lane >> 4;
   uint32_t w = first_wg + blockIdx.x;
   uint32_t n = quotient(w, by.Hkv);
   const uint32_t kvh = w - n * by.Hkv.d;
@@ -103,6 +104,7 @@ __global__ __launch_bounds__(THREADS, 2) void q4_tiles_kernel(Q4Args a, TileDiv 
   };
   const int wg_free = seen_by_all(tile * ROWS), wave_free = seen_by_all(tile * ROWS + wave * 16 * RB);
 
+  const bool busy = tile * ROWS + wave * 16 * RB < R;      // (the others put codes into LDS, no more)
   const float c = g.scale * LOG2E;
   const size_t rows0 = ((size_t)beta * g.Hkv + kvh) * (size_t)g.cap;
 
@@ -387,6 +389,17 @@ __global__ __launch_bounds__(THREADS, 2) void q4_tiles_kernel(Q4Args a, TileDiv 
 #pragma unroll
       for (int i = 0; i < PARTS; ++i) pA[b][i] = Vec{0, 0, 0, 0, 0, 0, 0, 0};
     barrier();
+    if (!busy) {
+      for (int t = 0; t < most_tiles; ++t) {
+        barrier();
+        const unsigned odd = t & 1 ? TILEB : 0;
+        if (t + 2 < n_tiles) file(Product<true>(), rk, odd);
+        if (t + 1 < n_tiles) file_v(rv, t + 1, 2 * TILEB + TILEB - odd);
+        if (t + 3 < n_tiles) request(rk, false, t + 3);
+        if (t + 2 < n_tiles) request(rv, true, t + 2);
+      }
+      return;
+    }
     if (n_tiles > 0) {
       score(sA, 0);
       score(sB, UNITB);
