@@ -1065,7 +1065,19 @@ static int phase2_q4_impl(const star_attn_shape* shape, const star_attn_rotary* 
   a.Vn = append && !rotary ? Vq : nullptr;
   a.O_sub = (float*)workspace;
   a.LSE_sub = (float*)workspace + rows * plan.s_total * g.d;
+  // One split of all keys: nothing to merge, and its workgroups store the results, unless what they are stored over is read by others.  (A workgroup has
+  // read its rows of Qq when it stores them.  A pair's split is stored as it is where its two parts need not lie one behind the other.)
+  const size_t es = shape->dtype == STAR_ATTN_F32 ? 4 : 2, q_bytes = (size_t)rows * g.d * es, k_bytes = (size_t)g.B * q_len * g.Hkv * g.d * es;
+  const auto read = [&](const void* x, size_t n) {
+    return overlap(x, n, Qq, q_bytes) || (append && (overlap(x, n, Kq, k_bytes) || overlap(x, n, Vq, k_bytes)));
+  };
+  const bool whole = plan.flat && plan.s_total == 1 &&
+                     (pair ? !plan.decode && !read(A, (size_t)rows * g.d * 4) && !read(LSE, (size_t)rows * 4)
+                           : O == Qq ? !append || (!overlap(O, q_bytes, Kq, k_bytes) && !overlap(O, q_bytes, Vq, k_bytes)) : !read(O, q_bytes));
+  a.O = whole && !pair ? O : nullptr;
+  if (whole && pair) { a.O_sub = A; a.LSE_sub = LSE; }
   if ((plan.decode ? launch_phase2_q4_stream(shape->dtype, a, st) : launch_phase2_q4_tiles(shape->dtype, a, st)) != hipSuccess) return STAR_ATTN_ERR_LAUNCH_FAILED;
+  if (whole) return STAR_ATTN_OK;
   MergeArgs m;
   m.g = g; m.plan = plan; m.wide = 0; m.keep_nan = 1;
   m.q_len = (int32_t)q_len; m.out_bf16 = shape->dtype == STAR_ATTN_BF16;

@@ -155,11 +155,11 @@ struct StreamCall {
 struct FlatStream {
   const void *Qq, *Kn, *Vn;
   Q4Rows q4;
-  float* O_sub;
+  void* out;                    // O, or O_sub with LSE_sub behind it
   int32_t cache_len, cap;
   uint32_t heads, rows;         // G << 16 | Hkv, q_len << 16 | splits
   float scale;
-  int32_t batch_causal;         // B << 1 | causal
+  int32_t batch_kind;           // B << 2 | whether `out` is O << 1 | causal
   uint32_t m[4];                // the divisors'
   uint32_t first_wg;
 };
@@ -170,14 +170,15 @@ template <int D>
 __device__ __forceinline__ StreamCall unpacked(const FlatStream& c) {
   StreamCall x;
   Geom& g = x.a.g;
-  g.B = c.batch_causal >> 1; g.G = c.heads >> 16; g.Hkv = c.heads & 0xffff; g.Hq = g.G * g.Hkv; g.d = D;
+  g.B = c.batch_kind >> 2; g.G = c.heads >> 16; g.Hkv = c.heads & 0xffff; g.Hq = g.G * g.Hkv; g.d = D;
   g.L = g.b = g.a = 0; g.cap = c.cap; g.scale = c.scale;
   const int splits = c.rows & 0xffff;
   x.a.plan = SplitPlan{0, 0, 0, 0, splits, 1, 1, 0, 0};
-  x.a.cache_len = c.cache_len; x.a.q_len = c.rows >> 16; x.a.causal = c.batch_causal & 1;
+  x.a.cache_len = c.cache_len; x.a.q_len = c.rows >> 16; x.a.causal = c.batch_kind & 1;
   x.a.Qq = c.Qq; x.a.Kn = c.Kn; x.a.Vn = c.Vn; x.a.q4 = c.q4;
-  x.a.O_sub = c.O_sub;
-  x.a.LSE_sub = c.O_sub + (size_t)g.B * splits * g.Hq * x.a.q_len * D;
+  x.a.O = c.batch_kind & 2 ? c.out : nullptr;
+  x.a.O_sub = (float*)c.out;
+  x.a.LSE_sub = (float*)c.out + (size_t)g.B * splits * g.Hq * x.a.q_len * D;
   x.by = StreamDiv{div_of(g.Hkv, c.m[0]), div_of(splits, c.m[1]), div_of(g.G, c.m[2]), div_of(splits * WAVES, c.m[3])};
   x.first_wg = c.first_wg;
   return x;
@@ -498,7 +499,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void q4_stream_kernel(C call) {
 #pragma unroll
     for (int k = 0; k < WAVES; ++k) lt += lds_l[k][16 * b + qc] * __builtin_amdgcn_exp2f((lds_m[k][16 * b + qc] - mm) * c);
     const float scale = lt == 0.f ? 0.f : __builtin_amdgcn_exp2f((st.m[b] - mm) * c) * (1.f / lt);
-    if (threadIdx.x < 16 && live[b])
+    if (threadIdx.x < 16 && live[b] && !a.O)
       a.LSE_sub[out0 + (size_t)head[b] * a.q_len + j[b]] = lt == 0.f ? -INFINITY : (mm * c - (TOP - 3) + __builtin_amdgcn_logf(lt)) * LN2;
     float* mine = meet + wave * 16 * D + qc * D;
     if (b > 0) __syncthreads();
@@ -512,7 +513,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void q4_stream_kernel(C call) {
 #pragma unroll
       for (int k = 0; k < WAVES; ++k) acc += *(const f32x4*)(meet + k * 16 * D + r * D + (chunk ^ r) * 4);
       const int tj = (int)quotient(row, by.G);
-      *(f32x4*)(a.O_sub + (out0 + (size_t)(kvh * g.G + row - tj * g.G) * a.q_len + tj) * D + 4 * chunk) = acc;
+      const int h = kvh * g.G + row - tj * g.G;
+      if (a.O) store4((T*)a.O + (((size_t)beta * a.q_len + tj) * g.Hq + h) * D + 4 * chunk, acc);
+      else *(f32x4*)(a.O_sub + (out0 + (size_t)h * a.q_len + tj) * D + 4 * chunk) = acc;
     }
   }
 }
@@ -524,9 +527,9 @@ hipError_t launch_stream(const Q4Args& a, hipStream_t st) {
   const int64_t wgs = (int64_t)g.B * g.Hkv * a.plan.s_total;
   if (wgs > 0x7fffffff) return hipErrorInvalidValue;
   if (a.plan.flat) {
-    if (a.plan.s_total > 0xffff) return hipErrorInvalidValue;
-    FlatStream c = {a.Qq, a.Kn, a.Vn, a.q4, a.O_sub, (int32_t)a.cache_len, (int32_t)g.cap, (uint32_t)g.G << 16 | (uint32_t)g.Hkv,
-                    (uint32_t)a.q_len << 16 | (uint32_t)a.plan.s_total, g.scale, g.B << 1 | a.causal, {by.Hkv.m, by.splits.m, by.G.m, by.steps.m}, 0};
+    if (a.plan.s_total > 0xffff || (!a.O && a.LSE_sub != a.O_sub + (size_t)g.B * a.plan.s_total * g.Hq * a.q_len * D)) return hipErrorInvalidValue;
+    FlatStream c = {a.Qq, a.Kn, a.Vn, a.q4, a.O ? a.O : a.O_sub, (int32_t)a.cache_len, (int32_t)g.cap, (uint32_t)g.G << 16 | (uint32_t)g.Hkv,
+                    (uint32_t)a.q_len << 16 | (uint32_t)a.plan.s_total, g.scale, g.B << 2 | (a.O ? 2 : 0) | a.causal, {by.Hkv.m, by.splits.m, by.G.m, by.steps.m}, 0};
     return launch_in_pieces(wgs, 64 * WAVES, [&](unsigned first, unsigned n) {
       c.first_wg = first;
       q4_stream_kernel<T, D, PP, RB, NT, FlatStream><<<dim3(n), 64 * WAVES, 0, st>>>(c);

@@ -36,6 +36,12 @@ __device__ __forceinline__ void load8(const T* p, float (&x)[8]) {
   }
 }
 
+// Four elements of an output row in the storage type.
+__device__ __forceinline__ void store4(float* p, const f32x4& x) { *(f32x4*)p = x; }
+__device__ __forceinline__ void store4(__bf16* p, const f32x4& x) {
+  *(bf16x4*)p = bf16x4{(__bf16)x[0], (__bf16)x[1], (__bf16)x[2], (__bf16)x[3]};
+}
+
 // Eight codes times their unit.
 __device__ __forceinline__ bf16x8 values(uint32_t c, float unit) {
   const q4_bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, unit, 0), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, unit, 1);

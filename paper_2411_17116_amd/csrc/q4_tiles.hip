@@ -536,8 +536,15 @@ __global__ __launch_bounds__(THREADS, 2) void q4_tiles_kernel(Q4Args a, TileDiv 
     const int row = tile * ROWS + wave * 16 * RB + 16 * b + qc;
     if (row >= R) continue;
     const int j = (int)quotient(row, by.G);
-    const size_t out = out0 + (size_t)(kvh * g.G + row - j * g.G) * a.q_len + j;
+    const int h = kvh * g.G + row - j * g.G;
+    const size_t out = out0 + (size_t)h * a.q_len + j;
     const float inv = l[b] == 0.f ? 0.f : 1.f / l[b], up = down ? __builtin_ldexpf(1.f, DOWN) : 1.f;
+    if (a.O) {
+      T* o = (T*)a.O + (((size_t)beta * a.q_len + j) * g.Hq + h) * D + 4 * j4;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) store4(o + 16 * dt, r.o[b][dt] * inv * up);
+      continue;
+    }
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) *(f32x4*)(a.O_sub + out * D + 16 * dt + 4 * j4) = r.o[b][dt] * inv * up;
     if (j4 == 0) a.LSE_sub[out] = l[b] == 0.f ? -INFINITY : (r.ref[b] + __builtin_amdgcn_logf(l[b])) * LN2;

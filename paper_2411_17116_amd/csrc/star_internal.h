@@ -338,6 +338,7 @@ struct Q4Args {
   Q4Rows q4;
   float* O_sub;
   float* LSE_sub;
+  void* O;                // one split of all keys: the call's output [B, q_len, Hq, d] instead of O_sub and LSE_sub; else null
 };
 hipError_t launch_phase2_q4_stream(int dtype, const Q4Args& a, hipStream_t st);      // plan.decode
 hipError_t launch_phase2_q4_tiles(int dtype, const Q4Args& a, hipStream_t st);

@@ -188,10 +188,12 @@ CALLS = [
     # rows that fill 16, pass it, fill more
     ("bf16", 1, 8, 2, 128, 500, 4), ("bf16", 1, 8, 2, 128, 500, 5), ("bf16", 1, 16, 16, 128, 63, 16), ("bf16", 1, 16, 16, 128, 64, 17),
     ("bf16", 1, 20, 4, 128, 1001, 7), ("bf16", 2, 32, 8, 128, 3001, 33), ("bf16", 1, 32, 8, 128, 9001, 130), ("bf16", 1, 17, 1, 128, 77, 3),
+    ("bf16", 70, 8, 8, 128, 1000, 1), ("bf16", 70, 16, 8, 128, 65, 10), ("bf16", 40, 8, 8, 128, 700, 60),
     ("bf16", 1, 32, 8, 128, 20000, 8), ("bf16", 1, 32, 8, 128, 20000, 16), ("bf16", 1, 40, 1, 128, 40000, 1), ("bf16", 1, 8, 8, 128, 5, 300),
     # fp32
     ("fp32", 1, 1, 1, 64, 1, 1), ("fp32", 1, 1, 1, 64, 1024, 32), ("fp32", 2, 4, 2, 64, 203, 3), ("fp32", 1, 8, 2, 128, 5001, 37),
     ("fp32", 1, 8, 2, 128, 33, 1), ("fp32", 1, 5, 1, 128, 2100, 2), ("fp32", 1, 32, 8, 64, 20001, 1), ("fp32", 3, 6, 6, 128, 700, 50),
+    ("fp32", 70, 8, 8, 64, 500, 1), ("fp32", 40, 8, 8, 128, 300, 40),
 ]
 
 
@@ -380,11 +382,20 @@ def test_calls_on_two_streams():
         assert all(torch.equal(c.O, w) for c, w in zip(calls, want))
 
 
-def test_output_over_the_queries():
-    c = Call("bf16", 1, 8, 2, 128, 900, 6, seed=9)
+@pytest.mark.parametrize("dtype,B,Hq,Hkv,d,L,q", [("bf16", 1, 8, 2, 128, 900, 6), ("bf16", 70, 8, 8, 128, 90, 2), ("bf16", 3, 8, 8, 128, 100, 100),
+                                                  ("fp32", 70, 8, 8, 64, 200, 3)])
+@pytest.mark.parametrize("over", ["Q", "K", "V"])
+def test_output_over_what_is_read(dtype, B, Hq, Hkv, d, L, q, over):
+    """With many splits, and with one, whose workgroups store the output themselves."""
+    c = Call(dtype, B, Hq, Hkv, d, L, q, seed=9)
+    if over != "Q" and Hq != Hkv:
+        pytest.skip("sizes differ")
     want = c.appended()
-    Q = c.Q.clone()
-    sa.phase2_q4(c.shape, 900, Q, c.K, c.V, c.cache, Q, c.ws)
+    print(f"{dtype} {B} {Hq}/{Hkv} L={L} q={q} over {over}", flush=True)
+    Q, K, V = c.Q.clone(), c.K.clone(), c.V.clone()
+    O = {"Q": Q, "K": K, "V": V}[over]
+    sa.phase2_q4(c.shape, L, Q, K, V, c.cache, O, c.ws)
     torch.cuda.synchronize()
-    c.O = Q
+    assert all(torch.equal(x, y) for x, y in zip(c.tensors(), want))
+    c.O = O
     c.check_O(want)
