@@ -486,8 +486,20 @@ static bool make_q4_plan(const star_attn_shape* s, const Geom& g, int64_t q_len,
     x.n_blocks = (int32_t)n;
     int64_t splits = 0;
     if (!want_parts) {
-      const int64_t worth = ceil_div(total, min_len);
-      splits = want < worth ? want : worth;
+      int64_t worth = ceil_div(total, min_len), most = want;
+      const int64_t wgs = (int64_t)g.B * g.Hkv * ceil_div(rows, tile);
+      if (tile <= 32) {
+        // Two workgroups on a CU pay where each wavefront has four units or more, and the pairs to merge are few beside them.  us, two / one (32 / 8 heads): 8000
+        // keys 10.3 / 9.8, 16000 11.4 / 10.9, 24000 12.3 / 12.0, 32768 12.6 / 14.1, 131072 27.6 / 30.3; 32 rows on 16000 19.1 / 15.9, on 32768 18.6 / 19.5; one KV head,
+        // eight rows: 64000 12.0 / 10.4, 500000 (512 splits) 21.0 / 19.0; a million keys of eight heads 186 / 220.
+        const int64_t units = ceil_div(total, 4 * 32 * want);
+        if (want > 1 && !(units >= 4 && (want <= 128 || units >= 16))) most = want / 2;
+      } else if (wgs * (want < worth ? want : worth) < 64) {
+        // Few workgroups: one tile of keys to each half.  us, 256 / 128 keys: 80 rows on 1000 keys of eight heads 16.0 / 15.8 (32 workgroups), on 2000 (64)
+        // 16.9 / 17.4; fp32, 148 rows on 2000 of two (48) 17.0 / 14.7
+        worth = ceil_div(total, 128);
+      }
+      splits = most < worth ? most : worth;
       x.flat = 1;
       x.split_len = round_up(ceil_div(total, splits), unit);
       splits = ceil_div(total, x.split_len);
@@ -1111,7 +1123,7 @@ size_t star_attn_q4_workspace_bytes(const star_attn_shape* shape, int64_t max_q_
   // such number, for every tile that a call may take.
   const auto need = [&](int64_t q, int tile) {
     SplitPlan p = {};
-    const int64_t want = q4_splits(g, q, tile), worth = ceil_div(g.cap, q4_worth(tile));
+    const int64_t want = q4_splits(g, q, tile), worth = ceil_div(g.cap, 128);
     p.s_total = (int32_t)(want < worth ? want : worth);
     if (plan_bytes(shape, p, q) > best) best = plan_bytes(shape, p, q);
   };
