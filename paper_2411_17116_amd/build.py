@@ -16,7 +16,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libstarattn.so")
 SOURCES = ["api.hip", "rope.hip", "flash_f32.hip", "flash_bf16.hip",
-           "decode_bf16.hip", "merge.hip", "q4.hip", "q4_tiles.hip"]
+           "decode_bf16.hip", "merge.hip", "norm_rope.hip", "q4.hip",
+           "q4_tiles.hip"]
 # the benchmark's calibration kernels: a library of their own, so that the
 # product library holds nothing but the path
 CALIB_LIB = os.path.join(HERE, "libstarcalib.so")

@@ -21,36 +21,11 @@
 //     trips (nothing may be loaded ahead of a store that could alias it).
 // Measured: a decode token of the 32 / 8-head shape (48 rows) 2.6 us, where two kernels
 // that walked the heads in turn and a copy took 15 + 6 + 2.8 (and two more launch gaps).
-//
-// Query and key heads that are normed as well, positions on several axes, keys and values that go to a cache in
-// four bits: the same kernel (QkArgs).  The lanes that hold a row add up its squares, r = 1 / sqrt(mean x^2 + eps), and turn
-// x r w instead of x, all in fp32 with one rounding to the storage type; a four-bit row is made of the rounded values.
 #include "rotary.h"
-#include "q4.h"
 
 namespace star {
 
 namespace {
-
-typedef __attribute__((ext_vector_type(4))) float f32x4;
-typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
-
-template <typename T> struct Chunk;
-template <> struct Chunk<float> {
-  static constexpr int N = 4;
-  typedef f32x4 vec;
-  static __device__ __forceinline__ vec pack(const float (&x)[4]) { return f32x4{x[0], x[1], x[2], x[3]}; }
-};
-template <> struct Chunk<__bf16> {
-  static constexpr int N = 8;
-  typedef bf16x8 vec;
-  static __device__ __forceinline__ vec pack(const float (&x)[8]) {
-    bf16x8 v;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = (__bf16)x[e];      // round to nearest even
-    return v;
-  }
-};
 
 constexpr int THREADS = 256;
 constexpr int BATCH = 3;
@@ -70,26 +45,8 @@ struct RopeArgs {
   unsigned int* clear;    // eight counters to zero for the launch behind this one, or null
 };
 
-// What a launch does beyond that.
-enum { TURN = 0, NORM = 1, NORM_Q4 = 2 };
-struct NormArgs {
-  const int64_t* positions;     // [B, T, n_axes] or null: token t at pos0 + t
-  const void* q_norm;           // [d] or null
-  const void* k_norm;
-  uint64_t axis[2];             // two bits per frequency
-  float eps;
-  int16_t n_axes, cached;       // cached: keys go to rows of a cache (V's), else Kc is [B, T, Hkv, d]
-};
-struct NormQ4Args : NormArgs {
-  Q4Rows q4;                    // where K and V go
-};
-struct NoMore {};
-template <int MODE> struct More { typedef NormArgs type; };
-template <> struct More<TURN> { typedef NoMore type; };
-template <> struct More<NORM_Q4> { typedef NormQ4Args type; };
-
-template <typename T, int half, int TT, int MODE>
-__global__ __launch_bounds__(THREADS) void rope_kernel(RopeArgs a, typename More<MODE>::type more) {
+template <typename T, int half, int TT>
+__global__ __launch_bounds__(THREADS) void rope_kernel(RopeArgs a) {
   constexpr int N = Chunk<T>::N;
   typedef typename Chunk<T>::vec vec;
   __shared__ float cs_all[TT][half], sn_all[TT][half];
@@ -103,13 +60,8 @@ __global__ __launch_bounds__(THREADS) void rope_kernel(RopeArgs a, typename More
 #pragma unroll
     for (int k0 = 0; k0 < TT; k0 += THREADS / half) {
       const int k = k0 + tid / half;
-      if (k < TT) {                                // tokens past the last: angles nobody reads
-        int64_t pos = a.pos0 + (tok0 + k) % a.n_tokens;
-        if constexpr (MODE != TURN)
-          if (more.positions && tok0 + k < a.total)
-            pos = more.positions[(int64_t)(tok0 + k) * more.n_axes + (more.axis[i >> 5] >> (2 * (i & 31)) & 3)];
-        rotary_angle(pos, inv_freq, &cs_all[k][i], &sn_all[k][i]);
-      }
+      if (k < TT)                                  // tokens past the last: angles nobody reads
+        rotary_angle(a.pos0 + (tok0 + k) % a.n_tokens, inv_freq, &cs_all[k][i], &sn_all[k][i]);
     }
   }
   __syncthreads();
@@ -124,7 +76,7 @@ __global__ __launch_bounds__(THREADS) void rope_kernel(RopeArgs a, typename More
   const uint32_t beta = tok / a.n_tokens, t = tok % a.n_tokens;
   constexpr size_t d = 2 * half;
   const size_t cache0 = ((size_t)beta * a.Hkv * a.cap + a.dst_row + t) * d + c;
-  const int n_rows = a.H + (MODE == TURN || a.V ? 2 : 1) * a.Hkv;
+  const int n_rows = a.H + 2 * a.Hkv;
   for (int h0 = slot; h0 < n_rows; h0 += BATCH * n_slots) {
     vec lo[BATCH], hi[BATCH];
     T* dst[BATCH];
@@ -141,8 +93,6 @@ __global__ __launch_bounds__(THREADS) void rope_kernel(RopeArgs a, typename More
         const int g = h - a.H - (v ? a.Hkv : 0);
         src = (const T*)(v ? a.V : a.K) + ((size_t)tok * a.Hkv + g) * d + c;
         dst[u] = (T*)(v ? a.Vc : a.Kc) + cache0 + (size_t)g * a.cap * d;
-        if constexpr (MODE == NORM)
-          if (!v && !more.cached) dst[u] = (T*)a.Kc + ((size_t)tok * a.Hkv + g) * d + c;
       }
       lo[u] = *(const vec*)src;
       hi[u] = *(const vec*)(src + half);
@@ -152,40 +102,15 @@ __global__ __launch_bounds__(THREADS) void rope_kernel(RopeArgs a, typename More
       const int h = h0 + u * n_slots;
       if (h >= n_rows) break;
       if (h < a.H + a.Hkv) {
-        float ylo[N], yhi[N], xlo[N], xhi[N];
-#pragma unroll
-        for (int e = 0; e < N; ++e) { xlo[e] = (float)lo[u][e]; xhi[e] = (float)hi[u][e]; }
-        if constexpr (MODE != TURN) {
-          const T* norm = (const T*)(h < a.H ? more.q_norm : more.k_norm);
-          if (norm) {
-            const vec wlo = *(const vec*)(norm + c), whi = *(const vec*)(norm + half + c);
-            float sum = 0.f;
-#pragma unroll
-            for (int e = 0; e < N; ++e) sum = fmaf(xlo[e], xlo[e], fmaf(xhi[e], xhi[e], sum));
-#pragma unroll
-            for (int x = 1; x < cpr; x <<= 1) sum += __shfl_xor(sum, x);
-            const float r = 1.f / sqrtf(sum * (1.f / d) + more.eps);
-#pragma unroll
-            for (int e = 0; e < N; ++e) { xlo[e] = xlo[e] * r * (float)wlo[e]; xhi[e] = xhi[e] * r * (float)whi[e]; }
-          }
-        }
+        float ylo[N], yhi[N];
 #pragma unroll
         for (int e = 0; e < N; ++e) {
-          const float x = xlo[e], y = xhi[e];
+          const float x = (float)lo[u][e], y = (float)hi[u][e];
           ylo[e] = rotary_lo(x, y, cs[e], sn[e]);
           yhi[e] = rotary_hi(x, y, cs[e], sn[e]);
         }
         lo[u] = Chunk<T>::pack(ylo);
         hi[u] = Chunk<T>::pack(yhi);
-      }
-      if constexpr (MODE == NORM_Q4) {
-        if (h >= a.H) {
-          const bool v = h >= a.H + a.Hkv;
-          const size_t row = ((size_t)beta * a.Hkv + h - a.H - (v ? a.Hkv : 0)) * a.cap + a.dst_row + t;
-          q4_file<N, d>(v ? more.q4.v_codes : more.q4.k_codes, v ? more.q4.v_scales : more.q4.k_scales, row, c, lo[u]);
-          q4_file<N, d>(v ? more.q4.v_codes : more.q4.k_codes, v ? more.q4.v_scales : more.q4.k_scales, row, c + half, hi[u]);
-          continue;
-        }
       }
       *(vec*)dst[u] = lo[u];
       *(vec*)(dst[u] + half) = hi[u];
@@ -193,11 +118,11 @@ __global__ __launch_bounds__(THREADS) void rope_kernel(RopeArgs a, typename More
   }
 }
 
-template <typename T, int half, int TT, int MODE>
-hipError_t launch_tokens(RopeArgs a, const typename More<MODE>::type& more, hipStream_t st) {
+template <typename T, int half, int TT>
+hipError_t launch(RopeArgs a, hipStream_t st) {
   return launch_in_pieces(((int64_t)a.total + TT - 1) / TT, THREADS, [&](unsigned first, unsigned n_wgs) {
     a.first = first * TT;
-    rope_kernel<T, half, TT, MODE><<<dim3(n_wgs), THREADS, 0, st>>>(a, more);
+    rope_kernel<T, half, TT><<<dim3(n_wgs), THREADS, 0, st>>>(a);
     a.clear = nullptr;
   });
 }
@@ -208,17 +133,12 @@ hipError_t launch_tokens(RopeArgs a, const typename More<MODE>::type& more, hipS
 // tokens (a kernel that gave a thread all heads of its chunk, before): 32 rows 376 / 390 /
 // 413 (469), 16 rows 177 / 190 / 212 (240), 8 rows 92 / 76 / 81 (86), 4 rows 87 / 50 / 41
 // (44), 1 row 79 / 40 / 30 (35); 4000 tokens of 8 rows 8.6 / 7.5 / 7.6 (8.8).
-template <typename T, int half, int MODE>
-hipError_t launch(const RopeArgs& a, const typename More<MODE>::type& more, hipStream_t st) {
-  const int64_t rows = (int64_t)a.H + (MODE == TURN || a.V ? 2 : 1) * a.Hkv;
-  if (rows >= 16 || a.total < 1024) return launch_tokens<T, half, 1, MODE>(a, more, st);
-  if (rows > 4 || a.total < 4096) return launch_tokens<T, half, 4, MODE>(a, more, st);
-  return launch_tokens<T, half, 16, MODE>(a, more, st);
-}
-template <int MODE>
-hipError_t launch(int dtype, int d, const RopeArgs& a, const typename More<MODE>::type& more, hipStream_t st) {
-  if (dtype != 0) return launch<__bf16, 64, MODE>(a, more, st);
-  return d == 64 ? launch<float, 32, MODE>(a, more, st) : launch<float, 64, MODE>(a, more, st);
+template <typename T, int half>
+hipError_t launch(const RopeArgs& a, hipStream_t st) {
+  const int64_t rows = (int64_t)a.H + 2 * a.Hkv;
+  if (rows >= 16 || a.total < 1024) return launch<T, half, 1>(a, st);
+  if (rows > 4 || a.total < 4096) return launch<T, half, 4>(a, st);
+  return launch<T, half, 16>(a, st);
 }
 
 }  // namespace
@@ -235,24 +155,8 @@ hipError_t launch_rope(int dtype, const Geom& g, int H, const void* X, void* Y, 
   a.n_tokens = (uint32_t)n_tokens; a.total = (uint32_t)total;
   a.cap = g.cap; a.dst_row = dst_row; a.pos0 = pos0; a.log2_theta = log2(theta);
   a.clear = clear;
-  return launch<TURN>(dtype, g.d, a, NoMore{}, st);
-}
-
-hipError_t launch_qk(int dtype, const Geom& g, const QkArgs& q, hipStream_t st) {
-  const int64_t total = (int64_t)g.B * q.n_tokens;
-  if (total == 0) return hipSuccess;
-  if (total > 0x7fffffff) return hipErrorInvalidValue;
-  RopeArgs a;
-  a.X = q.Q; a.Y = q.Yq; a.K = q.K; a.V = q.V; a.Kc = q.Yk; a.Vc = q.Vc;
-  a.H = q.Q ? g.Hq : 0; a.Hkv = q.K ? g.Hkv : 0;
-  a.n_tokens = (uint32_t)q.n_tokens; a.total = (uint32_t)total;
-  a.cap = g.cap; a.dst_row = q.dst_row; a.pos0 = q.pos0; a.log2_theta = log2(q.theta);
-  a.clear = q.clear;
-  NormQ4Args m;
-  m.positions = q.positions; m.q_norm = q.q_norm; m.k_norm = q.k_norm; m.eps = q.eps; m.n_axes = (int16_t)q.n_axes;
-  m.axis[0] = q.axis[0]; m.axis[1] = q.axis[1]; m.cached = (int16_t)q.cached;
-  m.q4 = q.q4;
-  return q.q4.k_codes ? launch<NORM_Q4>(dtype, g.d, a, m, st) : launch<NORM>(dtype, g.d, a, m, st);
+  if (dtype != 0) return launch<__bf16, 64>(a, st);
+  return g.d == 64 ? launch<float, 32>(a, st) : launch<float, 64>(a, st);
 }
 
 }  // namespace star

@@ -49,6 +49,24 @@ __device__ __forceinline__ void rotary_angle(int64_t pos, double inv_freq, float
   *cs = (q + 1) & 2 ? -fc : fc;
 }
 
+// Rows of T as the kernels that rotate take them: 16 bytes at a time.
+template <typename T> struct Chunk;
+template <> struct Chunk<float> {
+  static constexpr int N = 4;
+  typedef __attribute__((ext_vector_type(4))) float vec;
+  static __device__ __forceinline__ vec pack(const float (&x)[4]) { return vec{x[0], x[1], x[2], x[3]}; }
+};
+template <> struct Chunk<__bf16> {
+  static constexpr int N = 8;
+  typedef __attribute__((ext_vector_type(8))) __bf16 vec;
+  static __device__ __forceinline__ vec pack(const float (&x)[8]) {
+    vec v;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = (__bf16)x[e];      // round to nearest even
+    return v;
+  }
+};
+
 // The pair (x, y) of dimensions i and i + d / 2.  Written out as it is rounded, so that every kernel
 // gives the same bits.
 __device__ __forceinline__ float rotary_lo(float x, float y, float cs, float sn) { return fmaf(x, cs, -(y * sn)); }
