@@ -361,8 +361,9 @@ int star_attn_rope(const star_attn_shape* shape, int32_t n_heads, int64_t n_toke
  * and then rotated as above, frequency i by the angle p_i * rope_theta^(-2i/d), where p_i is
  * the token's position on the axis that has frequency i (time, height and width of a
  * video's patch, for instance).  Sums, norms and the rotation run in fp32, angles in
- * double precision; the result is rounded once to the storage dtype.  Every element of
- * the row takes part, so a row that holds a NaN or an infinity comes out as NaN.
+ * double precision; the result is rounded once to the storage dtype.  A row that holds a
+ * NaN comes out as NaN; one that holds an infinity as NaN where that is rotated to, else
+ * as zeros.  A row of zeros is NaN where norm_eps is zero.
  */
 typedef struct star_attn_rotary {
   double rope_theta;         /* base of the frequencies, > 1 */

@@ -16,6 +16,8 @@ namespace star {
 
 namespace {
 
+#define INLINE __attribute__((always_inline))
+
 constexpr int THREADS = 256;
 
 template <bool Q4> struct Rows4 { Q4Rows q4; };      // where K and V go
@@ -117,12 +119,23 @@ __global__ __launch_bounds__(THREADS) void norm_rope_kernel(NormArgs<Q4> a) {
       for (int e = 0; e < N; ++e) { x[e] = (float)lo[e]; y[e] = (float)hi[e]; }
       if (h < a.H ? a.q_norm != nullptr : a.k_norm != nullptr) {
         const vec wlo = h < a.H ? q_norm[0] : k_norm[0], whi = h < a.H ? q_norm[1] : k_norm[1];
-        float sum = 0.f;
+        const auto mean_square = [&](float eps) INLINE {
+          float sum = 0.f;
 #pragma unroll
-        for (int e = 0; e < N; ++e) sum = fmaf(x[e], x[e], fmaf(y[e], y[e], sum));
+          for (int e = 0; e < N; ++e) sum = fmaf(x[e], x[e], fmaf(y[e], y[e], sum));
 #pragma unroll
-        for (int l = 1; l < cpr; l <<= 1) sum += __shfl_xor(sum, l);
-        const float r = 1.f / sqrtf(sum * (1.f / d) + a.eps);
+          for (int l = 1; l < cpr; l <<= 1) sum += __shfl_xor(sum, l);
+          return sum * (1.f / d) + eps;
+        };
+        float ms = mean_square(a.eps);
+        if (__builtin_expect(!(ms >= 0x1p-100f && ms < INFINITY), 0)) {
+          // (elements whose squares 32 bits do not hold: of 2^60 in size or, with an eps as small, of 2^-50)
+          const float f = ms < 1.f ? 0x1p100f : 0x1p-70f;
+#pragma unroll
+          for (int e = 0; e < N; ++e) { x[e] *= f; y[e] *= f; }
+          ms = mean_square(a.eps * f * f);
+        }
+        const float r = 1.f / sqrtf(ms);
 #pragma unroll
         for (int e = 0; e < N; ++e) { x[e] = x[e] * r * (float)wlo[e]; y[e] = y[e] * r * (float)whi[e]; }
       }

@@ -114,6 +114,100 @@ def test_rows_of_zeros_large_and_small_ones_and_nan():
     _near(Y, Q, w, 1e-6, torch.arange(6)[None, :, None].cuda(), [0] * 32, "fp32")
 
 
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("fp32", 64), ("fp32", 128)])
+@pytest.mark.parametrize("eps", [0.0, 1e-6])
+def test_rows_whose_squares_32_bits_do_not_hold(dtype, d, eps):
+    """Sizes from the storage type's largest to its least normal ones, in one workgroup; an infinity takes its row to zeros and,
+    where its pair is rotated to, NaN."""
+    gen = torch.Generator().manual_seed(21)
+    sizes = torch.tensor([2.0 ** e for e in (124, 80, 64, 58, 0, -45, -52, -60, -80, -110, -124)])
+    X = torch.rand(1, 3, len(sizes), d, generator=gen) + 0.5
+    X = (X * torch.sign(torch.randn(X.shape, generator=gen)) * sizes[:, None]).to(_dt(dtype)).cuda()
+    w = (1 + torch.randn(d, generator=gen) / 4).to(_dt(dtype)).cuda()
+    shape = sa.StarShape.make(dtype, 1, len(sizes), 1, d, 5, 5, 0, 5)
+    Y = torch.full_like(X, math.nan)
+    rotary = sa.Rotary(THETA, q_norm=w, eps=eps, pos0=3)
+    sa.qk_norm_rope(shape, rotary, X, None, Y, None)
+    torch.cuda.synchronize()
+    _near(Y, X, w, eps, torch.arange(3, 6)[None, :, None].cuda(), [0] * (d // 2), dtype)
+    X[0, 1, 4, 7] = math.inf
+    sa.qk_norm_rope(shape, rotary, X, None, Y, None)
+    torch.cuda.synchronize()
+    bad = Y.isnan()
+    assert bad.sum() == 2 and bad[0, 1, 4, 7] and bad[0, 1, 4, 7 + d // 2]
+    assert (Y[0, 1, 4][~bad[0, 1, 4]] == 0).all()
+
+
+def test_captured_and_replayed():
+    """The pass, both phases on projections and rows filed and read, captured together: replays among eager work give the
+    eager call's bits."""
+    L, q, Hq, Hkv, d = 900, 5, 8, 2, 128
+    Q, K, V, kw = _setup("bf16", 2, Hq, Hkv, d, L + q, 14, True)
+    shape = sa.StarShape.make("bf16", 2, Hq, Hkv, d, L, 300, 100, L + q)
+    cut = lambda X, lo, hi: X[:, lo:hi].clone()
+    positions = kw.pop("positions")
+    context, question = (sa.Rotary(THETA, positions=positions[:, s].contiguous(), **kw) for s in (slice(0, L), slice(L, None)))
+    first, then = [cut(X, 0, L) for X in (Q, K, V)], [cut(X, L, L + q) for X in (Q, K, V)]
+    work = [torch.empty_like(first[0]), torch.empty_like(then[0]), torch.empty_like(then[0])]
+    Kc, Vc = sa.alloc_cache(shape)
+    Kb, Vb = sa.alloc_cache(shape)
+    cache, O, Oq, O4 = sa.alloc_q4_cache(shape), torch.empty_like(first[0]), torch.empty_like(then[0]), torch.empty_like(then[0])
+    Yk, ws, ws2 = torch.empty_like(first[1]), sa.alloc_workspace(shape, q), sa.alloc_q4_workspace(shape, q)
+    out = [*work, Kc, Vc, Kb, Vb, cache.k_codes, cache.k_scales, cache.v_codes, cache.v_scales, O, Oq, O4, Yk]
+    ws1 = sa.alloc_workspace(shape, L)
+
+    def run():
+        work[0].copy_(first[0]), work[1].copy_(then[0]), work[2].copy_(then[0])
+        sa.qk_norm_rope(shape, context, None, first[1], None, Yk)
+        sa.phase1_norm_rope(shape, context, work[0], first[1], first[2], O, Kc, Vc, workspace=ws1)
+        sa.q4_store(shape, 0, L, Kc, Vc, cache)
+        sa.phase2_norm_rope(shape, question, L, work[1], then[1], then[2], Kc, Vc, Oq, ws)
+        sa.phase2_q4(shape, L, work[2], then[1], then[2], cache, O4, ws2, rotary=question)
+        sa.q4_load(shape, 0, L + q, cache, Kb, Vb)
+
+    for t in out:
+        t.zero_()
+    run()
+    torch.cuda.synchronize()
+    want = [t.clone() for t in out]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run()
+    for i in range(4):
+        for t in out:
+            t.fill_(7 * i + 1)
+        for t in (Kc, Vc, Kb, Vb):
+            t.zero_()
+        for t in out[7:11]:
+            t.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(out, want))
+
+
+def test_on_two_streams_at_once():
+    gen = torch.Generator().manual_seed(15)
+    shape = sa.StarShape.make("bf16", 1, 32, 8, 128, 5, 5, 0, 5)
+    w = torch.ones(128).bfloat16().cuda()
+    calls = [(_randn(gen, "bf16", 1, T, 32, 128), _randn(gen, "bf16", 1, T, 8, 128), sa.Rotary(THETA, q_norm=w, k_norm=w, pos0=T)) for T in (3000, 700)]
+    want, got = [], []
+    for Q, K, r in calls:
+        want.append((torch.empty_like(Q), torch.empty_like(K)))
+        got.append((torch.empty_like(Q), torch.empty_like(K)))
+        sa.qk_norm_rope(shape, r, Q, K, *want[-1])
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in calls]
+    for _ in range(5):
+        for (Q, K, r), y, s in zip(calls, got, streams):
+            y[0].zero_(), y[1].zero_()
+        torch.cuda.synchronize()
+        for (Q, K, r), y, s in zip(calls, got, streams):
+            sa.qk_norm_rope(shape, r, Q, K, *y, stream=s)
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, z) for a, b in zip(got, want) for x, z in zip(a, b))
+
+
 def _setup(dtype, B, Hq, Hkv, d, T, seed, pos=None):
     gen = torch.Generator().manual_seed(seed)
     Q, K, V = (_randn(gen, dtype, B, T, H, d) for H in (Hq, Hkv, Hkv))
@@ -185,6 +279,21 @@ def test_phase2_in_steps(dtype, B, Hq, Hkv, d, L, q, pos, q4):
     torch.cuda.synchronize()
     assert torch.equal(X, Yq)
     assert all(torch.equal(x, y) for x, y in zip(*outs))
+
+
+def test_elements_past_32_bits():
+    """Projections of 2^32 bytes and more: the last tokens, and those about 2^31 elements."""
+    T, Hq, d = 270000, 64, 128
+    shape = sa.StarShape.make("bf16", 1, Hq, 1, d, 5, 5, 0, 5)
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    Q = torch.randn(1, T, Hq, d, generator=gen, device="cuda", dtype=torch.bfloat16)
+    w = torch.ones(d).bfloat16().cuda()
+    Y = torch.empty_like(Q)
+    sa.qk_norm_rope(shape, sa.Rotary(THETA, q_norm=w), Q, None, Y, None)
+    torch.cuda.synchronize()
+    edge = 2 ** 31 // (Hq * d)
+    for t in (0, edge - 3, T - 6):
+        _near(Y[:, t:t + 6], Q[:, t:t + 6], w, 1e-6, torch.arange(t, t + 6)[None, :, None].cuda(), [0] * 64, "bf16")
 
 
 def test_a_serving_run():
