@@ -399,3 +399,79 @@ def test_output_over_what_is_read(dtype, B, Hq, Hkv, d, L, q, over):
     assert all(torch.equal(x, y) for x, y in zip(c.tensors(), want))
     c.O = O
     c.check_O(want)
+
+
+def _rows_of(c, q, tensors, b, h, j):
+    """Token j's row of a long call against the oracle, in units of its bound."""
+    B, Hq, Hkv, d = c.dims
+    g, n = h // (Hq // Hkv), c.cached + j + 1
+    K, V = (star_q4.values(tensors[i][b, g, :n], tensors[i + 1][b, g, :n]) for i in (0, 2))
+    A, lse, weights, size, total = star_q4.attend(c.Q[b, j:j + 1, h], K, V, c.scale)
+    bound = _bound("bf16", d, n, size, weights, total, 1) + A.abs() * 2.0 ** -8
+    return ((c.O[b, j:j + 1, h].double() - A).abs() / bound).max().item()
+
+
+@pytest.mark.parametrize("q", [1, 4200])
+def test_bytes_past_32_bits(q):
+    """64 sequences whose codes lie past 2^32 bytes, one token each and calls whose queries do as well."""
+    B, Hq, Hkv, d, L, cap = 64, 64, 8, 128, 70, 140000
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    rand = lambda *size: torch.randn(*size, generator=gen, device="cuda", dtype=torch.bfloat16)
+    c = Call.__new__(Call)
+    c.cached, c.q, c.dims, c.dtype, c.scale = L, q, (B, Hq, Hkv, d), "bf16", d ** -0.5
+    c.shape = sa.StarShape.make("bf16", B, Hq, Hkv, d, L, L, 0, cap)
+    c.Q, c.K, c.V, c.cache = rand(B, q, Hq, d), rand(B, q, Hkv, d), rand(B, q, Hkv, d), sa.alloc_q4_cache(c.shape)
+    assert c.cache.k_codes.numel() > 2 ** 32 and (q == 1 or c.Q.numel() > 2 ** 31)
+    Kc, Vc = rand(B, Hkv, L, d), rand(B, Hkv, L, d)
+    sa.q4_store(c.shape, 0, L, Kc, Vc, c.cache)
+    c.O = torch.full_like(c.Q, math.nan)
+    ws = torch.empty(sa.phase2_q4_plan(c.shape, L, q).workspace_bytes, dtype=torch.uint8, device="cuda")
+    sa.phase2_q4(c.shape, L, c.Q, c.K, c.V, c.cache, c.O, ws)
+    Kb, Vb = torch.empty_like(Kc), torch.empty_like(Vc)
+    sa.q4_load(c.shape, 0, L, c.cache, Kb, Vb)
+    torch.cuda.synchronize()
+    tensors = c.tensors()
+    for b in (0, 31, B - 1):
+        for plain, back, new, i in ((Kc, Kb, c.K, 0), (Vc, Vb, c.V, 2)):
+            codes, scales = star_q4.quantise(torch.cat([plain[b], new[b].transpose(0, 1)], 1))
+            assert torch.equal(tensors[i][b, :, :L + q], codes) and torch.equal(tensors[i + 1][b, :, :L + q], scales)
+            assert torch.equal(back[b].double(), star_q4.values(codes[:, :L], scales[:, :L]))
+            assert (tensors[i][b, :, L + q:L + q + 99] == 0).all()
+        for h, j in ((0, 0), (Hq - 1, q - 1), (9, q // 2)):
+            assert _rows_of(c, q, tensors, b, h, j) <= 1, (b, h, j)
+
+
+@pytest.mark.parametrize("q", [1, 20, 40, 300])
+def test_a_cache_of_one_head_past_32_bits(q):
+    """70 million keys, zeros but for some at the end and at both sides of byte 2^31 and 2^32 of the codes."""
+    d, L = 128, 70000000
+    shape = sa.StarShape.make("bf16", 1, 1, 1, d, L, L, 0, L + q)
+    cache = sa.alloc_q4_cache(shape)
+    assert cache.k_codes.numel() > 2 ** 32
+    cache.k_scales.fill_(127), cache.v_scales.fill_(127)
+    gen = torch.Generator().manual_seed(q)
+    Q, K, V = (_randn(gen, "bf16", 1, q, 1, d) for _ in range(3))
+    Q = Q * 4
+    spots, n = [2 ** 31 // 64 - 40, 2 ** 32 // 64 - 40, L - 80], 80
+    plain = [_randn(gen, "bf16", 1, 1, n, d) for _ in range(6)]
+    for i, at in enumerate(spots):
+        sa.q4_store(shape, at, n, plain[2 * i], plain[2 * i + 1], cache, plain_row=0)
+    O = torch.full_like(Q, math.nan)
+    sa.phase2_q4(shape, L, Q, K, V, cache, O, sa.alloc_q4_workspace(shape, q))
+    A, LSE = torch.empty(1, 1, q, d).cuda(), torch.empty(1, 1, q).cuda()
+    sa.phase2_q4_partial(shape, L, Q, cache, A, LSE, sa.alloc_q4_workspace(shape, q))
+    torch.cuda.synchronize()
+    k, v = (star_q4.values(*star_q4.quantise(torch.cat([*(x[0, 0] for x in plain[i::2]), X[0, :, 0]]))) for i, X in ((0, K), (1, V)))
+    assert torch.equal(star_q4.values(cache.v_codes[0, 0, L:], cache.v_scales[0, 0, L:]), v[3 * n:])
+    zeros = L - 3 * n
+    for j in (0, q // 2, q - 1):
+        x = Q[0, j, 0].double()
+        for last, got, half in ((3 * n + j + 1, O[0, j, 0], 2.0 ** -8), (3 * n, A[0, 0, j], 2.0 ** -16)):
+            s = k[:last] @ x * d ** -0.5
+            size = (k[:last].abs() @ x.abs()).max() * d ** -0.5
+            lse = torch.logsumexp(torch.cat([s, torch.tensor([math.log(zeros)], dtype=torch.float64).cuda()]), 0)
+            p = torch.exp(s - lse)
+            want, weights, total = p @ v[:last], p @ v[:last].abs(), v[:last].abs().sum(0)
+            bound = _bound("bf16", d, L, size[None], weights[None], total[None], 1 if half > 1e-3 else 2)[0] + want.abs() * (half if half > 1e-3 else 2.0 ** -24)
+            assert ((got.double() - want).abs() <= bound).all(), (j, last)
+        assert abs(LSE[0, 0, j].double() - lse) <= 2.0 ** -24 * (2 * (d + 4) * size + L / 32 + 64 + 8 * lse.abs())
