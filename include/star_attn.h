@@ -453,7 +453,8 @@ int star_attn_q4_load(const star_attn_shape* shape, int64_t first_row, int64_t n
  *   workspace  at least star_attn_q4_workspace_bytes(shape, q_len) bytes, 256-byte aligned
  * Other arguments, outputs (O_part, LSE_part, O) and errors as in star_attn_phase2.
  * star_attn_phase2_q4_partial: star_attn_phase2_partial over a four-bit cache, one host's pair
- * (A, LSE) for star_attn_merge; Kq and Vq both NULL for a context host.
+ * (A, LSE) for star_attn_merge; Kq and Vq both NULL for a context host.  (A row whose LSE is NaN
+ * counts as empty there, as every NaN log-sum-exp does.)
  * star_attn_phase2_q4_plan: what a star_attn_phase2_q4 call would run (see star_attn_phase2_plan).
  */
 size_t star_attn_q4_workspace_bytes(const star_attn_shape* shape, int64_t max_q_len);

@@ -7,6 +7,8 @@
 //     u + 1, the exponentials of unit u and the products of unit u - 1, which do not wait for each other.
 //   * The reference of a row's exponentials is a whole power of two that moves where a weight would pass 2^15: what has been summed up so far, and the weights
 //     of the unit on its way, are then multiplied by a power of two, which loses nothing, in a branch of its own.
+// 256 tokens of 32 / 8 heads on 131072 keys, 5.5e11 flops: 452 to 475 us, 1.2 PFLOP/s, with weights in one part; 615 to 715 in two (8.2e11 flops with the part more, 1.15 to
+// 1.3 PFLOP/s), where the matrix instructions are busy for 62 % of the cycles at 1.9 GHz.  A large library product reaches 1.34 to 1.38.
 #include "q4_attend.h"
 
 #include <type_traits>
