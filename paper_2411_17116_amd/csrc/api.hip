@@ -464,6 +464,16 @@ static int64_t q4_splits(const Geom& g, int64_t q_len, int tile) {
   return wgs < resident ? resident / wgs : 1;
 }
 static int64_t q4_worth(int tile) { return tile <= 32 ? 128 : 256; }
+// More splits than that, where they even out rounds of resident workgroups.  us, 32 / 8 heads.  Of a stream with more workgroups than one round three, if what the last round
+// leaves idle outweighs what the pairs cost, one / three splits: 65 sequences of 4000 keys 70 / 62, 66 of 8000 133 / 109, 70 of 60000 964 / 761, 100 of 16000 317 / 293, eight tokens, 70 of 30000 502 / 455; but 100 of
+// 4000 84 / 84 (with four tokens 84 / 98), 65 of 2000 36 / 36, 1000 23.7 / 26.6, 66 of 3500 with seven 76 / 83, 256 of 8000 365 / 384.  Of row tiles up to four, by q4_cost, one / three: ten
+// sequences, 128 tokens on 32768 902 / 654, 20, 64 tokens on 8000 227 / 186, 40, 20 tokens on 8000 264 / 219; as long as the workgroups are four rounds at most, which bounds the workspace.
+static bool q4_stream_uneven(int64_t wgs, int tile, int64_t total) {
+  if (wgs <= 512) return false;
+  const double rounds = wgs / 512.0, idle = wgs % 512 ? 1 - wgs % 512 / 512.0 : 0;
+  return idle * total > 2000 * rounds * (tile / 16);
+}
+static bool q4_tiles_more(int64_t wgs, int64_t splits) { return splits <= 4 && wgs * splits <= 4 * 256; }
 // Time of a row-tiled call, in hundredths of that of 64 keys: rounds of resident workgroups, each its keys and what it takes to start and to store; and
 // the per-split pairs.
 static double q4_cost(const Geom& g, int64_t q_len, int tile, bool low, int64_t splits, int64_t len) {
@@ -477,7 +487,8 @@ static bool make_q4_plan(const star_attn_shape* s, const Geom& g, int64_t q_len,
   if (n > (1 << 24)) return false;
   double least = 0;
   bool found = false;
-  for (int i = 0; i < tiles.n; ++i) {
+  // `more`: 0 for as many splits as one round takes, else that many
+  for (int i = 0; i < tiles.n; ++i) for (int64_t more = 0; more <= (tiles.n == 1 || want_parts ? 0 : 4); ++more) {
     SplitPlan x = {};
     const int tile = tiles.rows[i];
     const int64_t want = q4_splits(g, q_len, tile), min_len = q4_worth(tile), unit = tile <= 32 ? 32 : 64;
@@ -488,12 +499,15 @@ static bool make_q4_plan(const star_attn_shape* s, const Geom& g, int64_t q_len,
     if (!want_parts) {
       int64_t worth = ceil_div(total, min_len), most = want;
       const int64_t wgs = (int64_t)g.B * g.Hkv * ceil_div(rows, tile);
+      if (more != 0 && (more <= want || more > worth || !q4_tiles_more(wgs, more))) continue;
+      if (more != 0) most = more;
       if (tile <= 32) {
         // Two workgroups on a CU pay where each wavefront has four units or more, and the pairs to merge are few beside them.  us, two / one (32 / 8 heads): 8000
         // keys 10.3 / 9.8, 16000 11.4 / 10.9, 24000 12.3 / 12.0, 32768 12.6 / 14.1, 131072 27.6 / 30.3; 32 rows on 16000 19.1 / 15.9, on 32768 18.6 / 19.5; one KV head,
         // eight rows: 64000 12.0 / 10.4, 500000 (512 splits) 21.0 / 19.0; a million keys of eight heads 186 / 220.
         const int64_t units = ceil_div(total, 4 * 32 * want);
         if (want > 1 && !(units >= 4 && (want <= 128 || units >= 16))) most = want / 2;
+        if (q4_stream_uneven(wgs, tile, total)) most = 3;
       } else if (wgs * (want < worth ? want : worth) < 64) {
         // Few workgroups: one tile of keys to each half.  us, 256 / 128 keys: 80 rows on 1000 keys of eight heads 16.0 / 15.8 (32 workgroups), on 2000 (64)
         // 16.9 / 17.4; fp32, 148 rows on 2000 of two (48) 17.0 / 14.7
@@ -1123,7 +1137,10 @@ size_t star_attn_q4_workspace_bytes(const star_attn_shape* shape, int64_t max_q_
   // such number, for every tile that a call may take.
   const auto need = [&](int64_t q, int tile) {
     SplitPlan p = {};
-    const int64_t want = q4_splits(g, q, tile), worth = ceil_div(g.cap, 128);
+    const int64_t wgs = (int64_t)g.B * g.Hkv * ceil_div((int64_t)g.G * q, tile), worth = ceil_div(g.cap, 128);
+    int64_t want = q4_splits(g, q, tile);
+    for (int64_t n = 2; n <= 4; ++n)
+      if (n > want && (tile > 32 ? q4_tiles_more(wgs, n) : n == 3 && q4_stream_uneven(wgs, tile, g.cap))) want = n;
     p.s_total = (int32_t)(want < worth ? want : worth);
     if (plan_bytes(shape, p, q) > best) best = plan_bytes(shape, p, q);
   };
@@ -1142,6 +1159,8 @@ size_t star_attn_q4_workspace_bytes(const star_attn_shape* shape, int64_t max_q_
       consider(tile == 16 && q > 16 / g.G ? 16 / g.G : q);
       consider(tile == 32 && half > 32 / g.G ? 32 / g.G : half);
     }
+  for (int tile = 64; tile <= 256; tile *= 2)
+    for (int64_t n = 2; n <= 4; ++n) consider(4 * 256 / n / pairs * tile / g.G);
   consider(16 / g.G);
   consider(32 / g.G);
   consider(max_q_len);

@@ -239,6 +239,26 @@ def test_parts(dtype, Hq, Hkv, d, L, block, q, more):
         c.check_pair(want, Op[:, m], Lp[:, m], True, lo=lo, hi=hi)
 
 
+@pytest.mark.parametrize("dtype,B,Hq,Hkv,d,L,q,splits,tile", [
+    ("bf16", 66, 8, 8, 128, 2300, 1, 3, 16), ("bf16", 66, 16, 8, 128, 4400, 13, 3, 32), ("fp32", 65, 8, 8, 64, 2200, 2, 3, 16),
+    ("bf16", 10, 32, 8, 128, 6000, 128, 3, 256), ("fp32", 40, 16, 4, 64, 3000, 30, 3, 128), ("bf16", 64, 8, 8, 128, 2000, 1, 1, 16)])
+def test_more_splits_than_a_round_takes(dtype, B, Hq, Hkv, d, L, q, splits, tile):
+    """More workgroups than one round, or most of one: rounds evened out by splits."""
+    c = Call(dtype, B, Hq, Hkv, d, L, q, seed=16)
+    p = sa.phase2_q4_plan(c.shape, L, q)
+    print(f"{dtype} {B} {Hq}/{Hkv} d={d} L={L} q={q}: {p.n_splits} of {p.tile_rows}", flush=True)
+    want = c.appended()
+    sa.phase2_q4(c.shape, L, c.Q, c.K, c.V, c.cache, c.O, c.ws)
+    A, LSE = torch.full((B, Hq, q, d), math.nan).cuda(), torch.full((B, Hq, q), math.nan).cuda()
+    sa.phase2_q4_partial(c.shape, L + q, c.Q, c.cache, A, LSE, c.ws)
+    torch.cuda.synchronize()
+    assert (p.n_splits, p.tile_rows) == (splits, tile)
+    assert all(torch.equal(x, y) for x, y in zip(c.tensors(), want))
+    c.check_O(want)
+    c.cached = L + q
+    c.check_pair(want, A, LSE, False)
+
+
 def test_pairs_of_two_hosts_merge_to_the_whole():
     whole = Call("bf16", 1, 8, 2, 128, 900, 5, seed=3)
     tensors, pairs = whole.appended(), []
