@@ -62,7 +62,7 @@ __global__ __launch_bounds__(THREADS, 2) void q4_tiles_kernel(Q4Args a, TileDiv 
   uint32_t n = quotient(w, by.Hkv);
   const uint32_t kvh = w - n * by.Hkv.d;
   w = quotient(n, by.tiles);
-  const uint32_t tile = n - w * by.tiles.d;
+  const uint32_t tile = by.tiles.d - 1 - (n - w * by.tiles.d);      // those that see most first
   n = quotient(w, by.splits);
   const uint32_t sp = w - n * by.splits.d, beta = n;
 
@@ -71,7 +71,11 @@ __global__ __launch_bounds__(THREADS, 2) void q4_tiles_kernel(Q4Args a, TileDiv 
   const int cached = a.Kn ? cache_len : total;
   int64_t lo64, hi64;
   split_range(a.plan, g.L, g.b, total, sp, &lo64, &hi64);
-  const int lo = (int)lo64, hi = (int)hi64;
+  // Keys up to what the tile's last row sees; the last tile of the rows sees all, and files the call's tokens.
+  // (us, 32 / 8 heads, 4096 tokens on 4000 keys: 634 with all keys for every tile, 535 so, 453 with the tiles that see most first; 300 of 20 sequences on 100 119 / 97 / 89)
+  const uint32_t last_row = (tile + 1) * ROWS < (uint32_t)R ? (tile + 1) * ROWS - 1 : R - 1;
+  const int seen = a.causal ? cache_len + (int)quotient(last_row, by.G) + 1 : total;
+  const int lo = (int)lo64, hi = hi64 < seen ? (int)hi64 : seen;
   const int all_tiles = hi > lo ? (hi - lo + KEYS - 1) / KEYS : 0;
   const int n_tiles = H == 1 ? all_tiles : (all_tiles - ring + 1) / 2, most_tiles = H == 1 ? all_tiles : (all_tiles + 1) / 2;
   const auto key_of = [&](int t) INLINE { return lo + KEYS * (H == 1 ? t : 2 * t + ring); };
@@ -163,7 +167,7 @@ __global__ __launch_bounds__(THREADS, 2) void q4_tiles_kernel(Q4Args a, TileDiv 
         raw.e = q4_unit(most);
 #pragma unroll
         for (int i = 0; i < E / 8; ++i) raw.c[i] = raw.e == 255u ? 0u : q4_codes(y[i], q4_unit_value(raw.e));
-        if (there && tile == 0) {
+        if (there && tile + 1 == by.tiles.d) {
           uint32_t* at = (uint32_t*)((unsigned char*)codes + (rows0 + key) * (D / 2) + my_col / 2);
 #pragma unroll
           for (int i = 0; i < E / 8; ++i) at[i] = raw.c[i];
