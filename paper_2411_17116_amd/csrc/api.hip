@@ -474,6 +474,18 @@ static bool q4_stream_uneven(int64_t wgs, int tile, int64_t total) {
   return idle * total > 2000 * rounds * (tile / 16);
 }
 static bool q4_tiles_more(int64_t wgs, int64_t splits) { return splits <= 4 && wgs * splits <= 4 * 256; }
+// The splits of a call whose parts are wanted, by row tile.
+static int64_t q4_parts(const Geom& g, int64_t q_len, int tile, SplitPlan* x) {
+  const int64_t n = ceil_div(g.L, g.b), bmax = g.b < g.L ? g.b : g.L, worth = bmax / q4_worth(tile), most = worth > 1 ? worth : 1;
+  int64_t spb = ceil_div(q4_splits(g, q_len, tile), n);
+  if (spb > most) spb = most;
+  x->split_len = round_up(ceil_div(bmax, spb), tile <= 32 ? 32 : 64);
+  spb = ceil_div(bmax, x->split_len);
+  const int64_t st = g.cap > g.L ? ceil_div(g.cap - g.L, x->split_len) : 1;
+  x->spb = (int32_t)spb;
+  x->st = (int32_t)st;
+  return n * spb + st;
+}
 // Time of a row-tiled call, in hundredths of that of 64 keys: rounds of resident workgroups, each its keys and what it takes to start and to store; and
 // the per-split pairs.
 static double q4_cost(const Geom& g, int64_t q_len, int tile, bool low, int64_t splits, int64_t len) {
@@ -499,7 +511,11 @@ static bool make_q4_plan(const star_attn_shape* s, const Geom& g, int64_t q_len,
     if (!want_parts) {
       int64_t worth = ceil_div(total, min_len), most = want;
       const int64_t wgs = (int64_t)g.B * g.Hkv * ceil_div(rows, tile);
-      if (more != 0 && (more <= want || more > worth || !q4_tiles_more(wgs, more))) continue;
+      // One split has nothing to merge: a launch less.  us, runs of 128 keys / one split.  32 / 8 heads, one token: 250 keys 8.2 / 5.9, 500 8.2 / 6.9, 630 8.2 / 7.5, 1000
+      // 8.8 / 9.6; fp32, d = 128, 630 8.8 / 8.6, 760 8.7 / 9.3; 32 rows, 630 11.0 / 10.6, 760 11.0 / 11.3.  Row tiles: 9 tokens, 189 keys 12.2 / 10.3, 259 12.8 / 13.2; eight
+      // heads, 60 tokens, 240 13.4 / 10.9, 310 13.3 / 13.9; fp32, 64 tokens, 244 14.8 / 13.7, 314 13.6 / 15.4.
+      const bool few = total <= (tile <= 32 ? 640 : 256);
+      if (more != 0 && (few || more <= want || more > worth || !q4_tiles_more(wgs, more))) continue;
       if (more != 0) most = more;
       if (tile <= 32) {
         // Two workgroups on a CU pay where each wavefront has four units or more, and the pairs to merge are few beside them.  us, two / one (32 / 8 heads): 8000
@@ -513,21 +529,13 @@ static bool make_q4_plan(const star_attn_shape* s, const Geom& g, int64_t q_len,
         // 16.9 / 17.4; fp32, 148 rows on 2000 of two (48) 17.0 / 14.7
         worth = ceil_div(total, 128);
       }
-      splits = most < worth ? most : worth;
+      splits = few ? 1 : most < worth ? most : worth;
       x.flat = 1;
       x.split_len = round_up(ceil_div(total, splits), unit);
       splits = ceil_div(total, x.split_len);
     } else {
-      const int64_t bmax = g.b < g.L ? g.b : g.L, most = bmax / min_len > 1 ? bmax / min_len : 1;
-      int64_t spb = ceil_div(want, n);
-      if (spb > most) spb = most;
-      x.split_len = round_up(ceil_div(bmax, spb), unit);
-      spb = ceil_div(bmax, x.split_len);
-      const int64_t st = g.cap > g.L ? ceil_div(g.cap - g.L, x.split_len) : 1;
-      splits = n * spb + st;
+      splits = q4_parts(g, q_len, tile, &x);
       if (splits > (1 << 24)) continue;
-      x.spb = (int32_t)spb;
-      x.st = (int32_t)st;
     }
     x.s_total = (int32_t)splits;
     const double cost = tiles.n == 1 ? 0 : q4_cost(g, q_len, tile, i == 1, splits, x.split_len);
@@ -1092,13 +1100,13 @@ static int phase2_q4_impl(const star_attn_shape* shape, const star_attn_rotary* 
   a.O_sub = (float*)workspace;
   a.LSE_sub = (float*)workspace + rows * plan.s_total * g.d;
   // One split of all keys: nothing to merge, and its workgroups store the results, unless what they are stored over is read by others.  (A workgroup has
-  // read its rows of Qq when it stores them.  A pair's split is stored as it is where its two parts need not lie one behind the other.)
+  // read its rows of Qq when it stores them.)
   const size_t es = shape->dtype == STAR_ATTN_F32 ? 4 : 2, q_bytes = (size_t)rows * g.d * es, k_bytes = (size_t)g.B * q_len * g.Hkv * g.d * es;
   const auto read = [&](const void* x, size_t n) {
     return overlap(x, n, Qq, q_bytes) || (append && (overlap(x, n, Kq, k_bytes) || overlap(x, n, Vq, k_bytes)));
   };
   const bool whole = plan.flat && plan.s_total == 1 &&
-                     (pair ? !plan.decode && !read(A, (size_t)rows * g.d * 4) && !read(LSE, (size_t)rows * 4)
+                     (pair ? !read(A, (size_t)rows * g.d * 4) && !read(LSE, (size_t)rows * 4)
                            : O == Qq ? !append || (!overlap(O, q_bytes, Kq, k_bytes) && !overlap(O, q_bytes, Vq, k_bytes)) : !read(O, q_bytes));
   a.O = whole && !pair ? O : nullptr;
   if (whole && pair) { a.O_sub = A; a.LSE_sub = LSE; }
@@ -1141,7 +1149,9 @@ size_t star_attn_q4_workspace_bytes(const star_attn_shape* shape, int64_t max_q_
     int64_t want = q4_splits(g, q, tile);
     for (int64_t n = 2; n <= 4; ++n)
       if (n > want && (tile > 32 ? q4_tiles_more(wgs, n) : n == 3 && q4_stream_uneven(wgs, tile, g.cap))) want = n;
+    const int64_t parts = ceil_div(g.L, g.b) > (1 << 24) ? 0 : q4_parts(g, q, tile, &p);
     p.s_total = (int32_t)(want < worth ? want : worth);
+    if (parts > p.s_total && parts <= (1 << 24)) p.s_total = (int32_t)parts;
     if (plan_bytes(shape, p, q) > best) best = plan_bytes(shape, p, q);
   };
   const auto consider = [&](int64_t q) {
@@ -1149,8 +1159,6 @@ size_t star_attn_q4_workspace_bytes(const star_attn_shape* shape, int64_t max_q_
     if (q > max_q_len) q = max_q_len;
     const Q4Tiles tiles = q4_tiles(shape, (int64_t)g.G * q);
     for (int i = 0; i < tiles.n; ++i) need(q, tiles.rows[i]);
-    SplitPlan p;
-    if (make_q4_plan(shape, g, q, g.cap, true, &p) && plan_bytes(shape, p, q) > best) best = plan_bytes(shape, p, q);
   };
   const int64_t pairs = (int64_t)g.B * g.Hkv;
   for (int tile = 16; tile <= 256; tile *= 2)

@@ -149,7 +149,7 @@ struct StreamState {
 struct StreamDiv {
   Div Hkv, splits, G, steps;      // steps between two of a wavefront's (flat plans): splits times wavefronts
 };
-// What a launch is handed: packed under a flat plan (see FlatCall), else as it is.
+// What a launch is handed: packed under a flat plan (but for a pair that is stored as it is), else as it is.
 struct StreamCall {
   Q4Args a;
   StreamDiv by;
@@ -529,8 +529,9 @@ hipError_t launch_stream(const Q4Args& a, hipStream_t st) {
   const StreamDiv by = {make_div(g.Hkv), make_div(a.plan.s_total), make_div(g.G), make_div((uint32_t)a.plan.s_total * WAVES)};
   const int64_t wgs = (int64_t)g.B * g.Hkv * a.plan.s_total;
   if (wgs > 0x7fffffff) return hipErrorInvalidValue;
-  if (a.plan.flat) {
-    if (a.plan.s_total > 0xffff || (!a.O && a.LSE_sub != a.O_sub + (size_t)g.B * a.plan.s_total * g.Hq * a.q_len * D)) return hipErrorInvalidValue;
+  // (a pair that is stored as it is need not have its two parts one behind the other)
+  if (a.plan.flat && (a.O || a.LSE_sub == a.O_sub + (size_t)g.B * a.plan.s_total * g.Hq * a.q_len * D)) {
+    if (a.plan.s_total > 0xffff) return hipErrorInvalidValue;
     FlatStream c = {a.Qq, a.Kn, a.Vn, a.q4, a.O ? a.O : a.O_sub, (int32_t)a.cache_len, (int32_t)g.cap, (uint32_t)g.G << 16 | (uint32_t)g.Hkv,
                     (uint32_t)a.q_len << 16 | (uint32_t)a.plan.s_total, g.scale, g.B << 2 | (a.O ? 2 : 0) | a.causal, {by.Hkv.m, by.splits.m, by.G.m, by.steps.m}, 0};
     return launch_in_pieces(wgs, 64 * WAVES, [&](unsigned first, unsigned n) {

@@ -241,7 +241,10 @@ def test_parts(dtype, Hq, Hkv, d, L, block, q, more):
 
 @pytest.mark.parametrize("dtype,B,Hq,Hkv,d,L,q,splits,tile", [
     ("bf16", 66, 8, 8, 128, 2300, 1, 3, 16), ("bf16", 66, 16, 8, 128, 4400, 13, 3, 32), ("fp32", 65, 8, 8, 64, 2200, 2, 3, 16),
-    ("bf16", 10, 32, 8, 128, 6000, 128, 3, 256), ("fp32", 40, 16, 4, 64, 3000, 30, 3, 128), ("bf16", 64, 8, 8, 128, 2000, 1, 1, 16)])
+    ("bf16", 10, 32, 8, 128, 6000, 128, 3, 256), ("fp32", 40, 16, 4, 64, 3000, 30, 3, 128), ("bf16", 64, 8, 8, 128, 2000, 1, 1, 16),
+    # few keys: one split, stored as it is, and the next number of them
+    ("bf16", 2, 32, 8, 128, 639, 1, 1, 16), ("bf16", 1, 32, 8, 128, 640, 1, 6, 16), ("bf16", 1, 32, 8, 128, 633, 7, 1, 32), ("fp32", 1, 8, 2, 64, 300, 4, 1, 16),
+    ("bf16", 1, 32, 8, 128, 200, 56, 1, 128), ("bf16", 1, 8, 8, 128, 57, 200, 3, 128), ("fp32", 1, 8, 2, 128, 190, 66, 1, 64)])
 def test_more_splits_than_a_round_takes(dtype, B, Hq, Hkv, d, L, q, splits, tile):
     """More workgroups than one round, or most of one: rounds evened out by splits."""
     c = Call(dtype, B, Hq, Hkv, d, L, q, seed=16)
@@ -419,6 +422,21 @@ def test_output_over_what_is_read(dtype, B, Hq, Hkv, d, L, q, over):
     assert all(torch.equal(x, y) for x, y in zip(c.tensors(), want))
     c.O = O
     c.check_O(want)
+
+
+@pytest.mark.parametrize("L,q", [(100, 1), (60, 40), (3000, 2)])
+@pytest.mark.parametrize("over", ["Q", "K"])
+def test_pair_over_what_is_read(L, q, over):
+    """In fp32 a pair's outputs fit where its queries or keys were."""
+    c = Call("fp32", 2, 4, 4, 64, L, q, seed=17)
+    want = c.appended()
+    print(f"L={L} q={q} over {over}", flush=True)
+    X = {"Q": c.Q, "K": c.K}[over].clone()
+    A, LSE = X.view(2, 4, q, 64), torch.full((2, 4, q), math.nan).cuda()
+    sa.phase2_q4_partial(c.shape, L, X if over == "Q" else c.Q, c.cache, A, LSE, c.ws, Kq=X if over == "K" else c.K, Vq=c.V)
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(c.tensors(), want))
+    c.check_pair(want, A, LSE, True, few=8)
 
 
 def _rows_of(c, q, tensors, b, h, j):

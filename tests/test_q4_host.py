@@ -141,6 +141,18 @@ def test_the_workspace_asked_for_covers_every_call():
     assert sa.q4_workspace_bytes(_shape(head_dim=64), 4) == sa.q4_workspace_bytes(_shape(), 0) == 0
 
 
+@pytest.mark.parametrize("dtype,B,Hq,Hkv,d,L,block,tail,top", [
+    ("fp32", 9, 3, 1, 64, 4269, 814, 175, 175),       # parts: a shorter call takes the lower tile, whose splits are more
+    ("bf16", 10, 32, 8, 128, 32768, 4096, 300, 200), ("bf16", 66, 32, 8, 128, 8000, 8000, 9, 9), ("fp32", 20, 16, 4, 128, 9000, 9000, 100, 100)])
+def test_the_workspace_covers_calls_that_are_cut_finer(dtype, B, Hq, Hkv, d, L, block, tail, top):
+    s = sa.StarShape.make(dtype, B, Hq, Hkv, d, L, block, 0, L + tail)
+    have = sa.q4_workspace_bytes(s, top)
+    for q in range(1, top + 1):
+        for at in {L, L + tail - q}:
+            for parts in (False, True):
+                assert sa.phase2_q4_plan(s, at, q, parts).workspace_bytes <= have, (q, at, parts)
+
+
 # ------------------------------------------------------------------ the binding
 
 
