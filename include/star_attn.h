@@ -384,8 +384,8 @@ typedef struct star_attn_rotary {
  *   K, Yk      [B, n_tokens, Hkv, d]   Yk may be K; both may be NULL, if Q is not
  * star_attn_phase1_norm_rope / star_attn_phase2_norm_rope: star_attn_phase1_rope /
  * star_attn_phase2_rope with `rotary` in place of rope_theta and pos0.  A rotary out of
- * range is STAR_ATTN_ERR_INVALID_SHAPE, positions or weights that are not 16-byte aligned
- * are STAR_ATTN_ERR_MISALIGNED.
+ * range is STAR_ATTN_ERR_INVALID_SHAPE; positions that are not 8-byte aligned and weights that
+ * are not 16-byte aligned are STAR_ATTN_ERR_MISALIGNED.
  */
 int star_attn_qk_norm_rope(const star_attn_shape* shape, const star_attn_rotary* rotary, int64_t n_tokens,
                            const void* Q, const void* K, void* Yq, void* Yk, void* hip_stream);

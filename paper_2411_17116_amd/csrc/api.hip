@@ -574,7 +574,7 @@ static int validate_rotary(const star_attn_shape* s, const star_attn_rotary* r) 
   if (!(r->norm_eps >= 0.f) || isinf(r->norm_eps) || r->n_axes < 1 || r->n_axes > 4) return STAR_ATTN_ERR_INVALID_SHAPE;
   for (int i = 0; i < s->head_dim / 2; ++i)
     if (r->axis[i] >= r->n_axes) return STAR_ATTN_ERR_INVALID_SHAPE;
-  if (misaligned(r->positions) || misaligned(r->q_norm) || misaligned(r->k_norm)) return STAR_ATTN_ERR_MISALIGNED;
+  if (((uintptr_t)r->positions & 7u) || misaligned(r->q_norm) || misaligned(r->k_norm)) return STAR_ATTN_ERR_MISALIGNED;
   return STAR_ATTN_OK;
 }
 // What every launch_qk call takes from it; `pos0` of its first token.

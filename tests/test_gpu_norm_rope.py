@@ -68,6 +68,20 @@ def test_pass(dtype, B, T, Hq, Hkv, d, axes):
     assert torch.equal(X, Yq) and torch.equal(Z, Yk)
 
 
+def test_positions_of_any_token_of_a_longer_tensor():
+    """A decode step's positions cut out of a prompt's: whole numbers, not 16 bytes, apart."""
+    gen = torch.Generator().manual_seed(22)
+    every = torch.randint(0, 4000, (1, 20, 3), generator=gen).cuda()
+    Q = _randn(gen, "bf16", 1, 2, 4, 128)
+    shape = sa.StarShape.make("bf16", 1, 4, 2, 128, 5, 5, 0, 5)
+    axis = [i % 3 for i in range(64)]
+    for t in (1, 2, 7, 18):
+        Y = torch.empty_like(Q)
+        sa.qk_norm_rope(shape, sa.Rotary(THETA, positions=every[:, t:t + 2], axis=axis), Q, None, Y, None)
+        torch.cuda.synchronize()
+        _near(Y, Q, None, 0.0, every[:, t:t + 2], axis, "bf16")
+
+
 def test_axes_dealt_in_turn_and_four_of_them():
     gen = torch.Generator().manual_seed(1)
     Q, K = _randn(gen, "bf16", 2, 9, 4, 128), _randn(gen, "bf16", 2, 9, 2, 128)

@@ -66,7 +66,7 @@ def _rows(shape, load, row=0, n=1, K=0x1000, V=0x1000, rows=64, at=0, c=Q4):
     (dict(rope_theta=1.0), INVALID), (dict(rope_theta=float("inf")), INVALID), (dict(pos0=-1), INVALID), (dict(norm_eps=-1e-6), INVALID),
     (dict(norm_eps=float("nan")), INVALID), (dict(norm_eps=float("inf")), INVALID), (dict(n_axes=0), INVALID), (dict(n_axes=5), INVALID),
     (dict(axis=_axis(63, 1)), INVALID), (dict(n_axes=2, axis=_axis(0, 2)), INVALID),
-    (dict(positions=0x1008), MISALIGNED), (dict(q_norm=0x1004), MISALIGNED), (dict(k_norm=0x1002), MISALIGNED)])
+    (dict(positions=0x1004), MISALIGNED), (dict(q_norm=0x1004), MISALIGNED), (dict(k_norm=0x1002), MISALIGNED)])
 def test_a_rotary_out_of_range(kw, code):
     r = _rotary(**kw)
     assert _qk(_shape(), r) == _p1(_shape(), r) == _p2(_shape(), r) == _p4(_shape(), r) == code
